@@ -39,7 +39,8 @@ KERNEL = "psa_pair_kernel<128, 128, 1, true, false>"    # the sparse attention a
 KERNEL_3D = "psa_pair_kernel<128, 128, 1, true, true>"  # ... with the 3D-padding masks
 ATTN_PREFIXES = ("psa_pair_kernel<", "psa_split_kernel<")  # attention kernels
 COUNTERS_MD = os.path.join(ROOT, "profiles", "psa_pair_kernel_wan14b_counters.md")
-SOURCES = ("paper_2609_37001_amd/csrc/psa_kernels.hip", "paper_2609_37001_amd/csrc/psa_launch.h",
+SOURCES = ("paper_2609_37001_amd/csrc/psa_kernels.hip", "paper_2609_37001_amd/csrc/psa_tile.h",
+           "paper_2609_37001_amd/csrc/psa_launch.h",
            "paper_2609_37001_amd/csrc/psa_api.hip", "paper_2609_37001_amd/build.py", "include/psa.h")
 WORKLOAD_TEXT = {
     "tiny": "tiny layer: B=1, 2 heads, d=64, grid 4x16x16 (N=1024), block 64, stripes drawn uniformly "
