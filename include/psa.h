@@ -303,6 +303,78 @@ psa_status_t psa_l2_distance(const void* o, const void* ref, int32_t batch_heads
                              int32_t head_dim, double* sq_err, double* sq_ref, void* workspace,
                              size_t workspace_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Norms and rotary positions of queries and keys: the step between a layer's projections and its
+ * attention.  Each row (token, head) x of head_dim channels becomes
+ *   n = x / sqrt(mean(x^2) + eps) * weight       (or x itself without a norm)
+ *   y = n with each channel pair of the video tokens turned by its angle
+ * with pair j of an axis of d_a channels turned by pos_a * theta^(-2 j / d_a), a = time, height, width,
+ * pos = origin + the token's place in the F x H x W grid.  Text tokens, behind the video, are not turned,
+ * nor are channels behind the three axes'.  The first axis has the first pairs.  Angles are formed in
+ * 64 bits, the rest in fp32; y is rounded to bf16 once.
+ * --------------------------------------------------------------------------------------------- */
+
+typedef enum {
+  PSA_TYPE_BF16 = 0,
+  PSA_TYPE_FP32 = 1
+} psa_type_t;
+
+typedef enum {
+  PSA_PAIRS_ADJACENT = 0, /* pair j: channels 2j and 2j + 1 */
+  PSA_PAIRS_HALVES = 1    /* pair j: channels j and j + head_dim / 2; the axes then fill the head */
+} psa_pairs_t;
+
+/* Rows of one tensor, [batch][n_heads][N][head_dim] by strides in elements (the channels of a row lie side
+ * by side).  16-byte aligned, the strides multiples of 16 bytes; a stride of 0 repeats rows (inputs only). */
+typedef struct {
+  void* x;
+  int64_t stride_b, stride_h, stride_n;
+  int32_t n_heads;
+} psa_rows_t;
+
+/* The rotation: N = frames * height * width + n_text tokens; channels of each axis (even, >= 0, together
+ * at most head_dim); theta > 0. */
+typedef struct {
+  psa_grid_t grid;
+  int32_t origin_t, origin_h, origin_w;
+  int32_t axis_t, axis_h, axis_w;
+  int32_t pairs;              /* psa_pairs_t */
+  double theta;
+} psa_rope_t;
+
+/* Queries and keys from the projection's rows to the attention's layout.
+ *   q, k          rows of x in type `type` (psa_type_t); k NULL: queries alone
+ *   q_out, k_out  device bf16 [batch][n_heads][N][head_dim], contiguous, 16-byte aligned; must not overlap
+ *                 any input
+ *   norm          0: the rotation alone (the weights must be NULL)
+ *   q_weight, k_weight  device fp32 [head_dim] each, or NULL for ones
+ *   eps           >= 0, finite
+ * head_dim 64 or 128; batch * tensors <= 65535. */
+psa_status_t psa_qk_norm_rope_fwd(const psa_rows_t* q, const psa_rows_t* k, void* q_out, void* k_out,
+                                  int32_t type, int32_t batch, int32_t head_dim, const psa_rope_t* rope,
+                                  int32_t norm, const float* q_weight, const float* k_weight, float eps,
+                                  hipStream_t stream);
+
+/* Bytes of device workspace of psa_qk_norm_rope_bwd (0 if invalid, or if there is no norm). */
+size_t psa_qk_norm_rope_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, psa_grid_t grid, int32_t norm);
+
+/* Gradients of psa_qk_norm_rope_fwd.
+ *   dq_out, dk_out  gradients of q_out and k_out, in their layout (bf16)
+ *   q, k            the forward's rows (without a norm their x may be NULL); k NULL: queries alone
+ *   dq, dk          rows that receive the gradients, in type `type`, strides of their own (none 0 where
+ *                   there is more than one row to write)
+ *   dq_weight, dk_weight  device fp32 [head_dim], written: with a norm required (whether the weights were
+ *                   NULL or not), without one ignored
+ *   workspace       device, psa_qk_norm_rope_workspace_size() bytes, 256-byte aligned (NULL without a norm)
+ * Sums over rows are in fp32 within a workgroup and in fp64 over workgroups, in a fixed order. */
+psa_status_t psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const psa_rows_t* q,
+                                  const psa_rows_t* k, const psa_rows_t* dq, const psa_rows_t* dk,
+                                  float* dq_weight, float* dk_weight, int32_t type, int32_t batch,
+                                  int32_t head_dim, const psa_rope_t* rope, int32_t norm,
+                                  const float* q_weight, const float* k_weight, float eps, void* workspace,
+                                  size_t workspace_bytes, hipStream_t stream);
+
 /* Static description of a status code. */
 const char* psa_status_string(psa_status_t status);
 

@@ -18,6 +18,10 @@ is no CPU or PyTorch fallback.
     qb, kb, vb = (to_blocks(x, grid, pb) for x in (q, k, v))
     ob = attention_fwd_3d(qb, kb, vb, grid, pb, params, tile=128)
     o = from_blocks(ob, grid, pb)
+
+Norms and 3D rotary positions of queries and keys, from the projection's [batch, N, heads, d]:
+
+    q, k = qk_norm_rope(xq.transpose(1, 2), xk.transpose(1, 2), grid, (44, 42, 42), q_weight=wq, k_weight=wk)
 """
 import contextlib
 import math
@@ -28,7 +32,7 @@ from ._lib import STRIDE_INF, PsaError  # noqa: F401
 __all__ = ["STRIDE_INF", "PsaError", "num_blocks", "workspace_size", "build_blockmap",
            "attention_fwd", "attention_fwd_noalloc", "plan", "run", "dense_fwd", "dense_workspace_size", "Workspace", "library_path",
            "blocked_tokens", "to_blocks", "from_blocks", "build_blockmap_3d", "plan_3d", "run_3d",
-           "attention_fwd_3d", "l2_distance"]
+           "attention_fwd_3d", "l2_distance", "qk_norm_rope", "qk_norm_rope_bwd"]
 
 
 def library_path():
@@ -429,3 +433,141 @@ def l2_distance(o, ref, sq_err=None, sq_ref=None, workspace=None, stream=None):
         _lib.check(_lib.lib().psa_l2_distance(_ptr(o), _ptr(ref), b * h, n, d, _ptr(err), _ptr(rref),
                                               _ptr(ws), ws.numel(), _stream(None, o.device)))
     return err, rref
+
+
+# ---------------------------------------------------------------------------------------------
+# Norms and rotary positions of queries and keys (include/psa.h, fourth part).
+# ---------------------------------------------------------------------------------------------
+
+def _rows(x, name, dtype, tokens, like=None):
+    """psa_rows_t of x, [batch, heads, N, head_dim] of any strides with the channels side by side."""
+    torch = _torch()
+    if dtype not in (torch.bfloat16, torch.float32) or x.dtype != dtype:
+        raise TypeError("%s must be bfloat16 or float32, queries and keys alike" % name)
+    if not x.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    if x.dim() != 4 or x.stride(3) != 1:
+        raise ValueError("%s must be [batch, heads, N, head_dim] with contiguous channels" % name)
+    if x.shape[2] != tokens:
+        raise ValueError("%s has %d tokens, the grid %d" % (name, x.shape[2], tokens))
+    if like is not None and (x.device != like.device or x.shape[0] != like.shape[0] or x.shape[3] != like.shape[3]):
+        raise ValueError("%s must share the queries' batch, head_dim and device" % name)
+    b, h, n = (s if size > 1 else 0 for s, size in zip(x.stride()[:3], x.shape))
+    return _lib.Rows(x.data_ptr(), b, h, n, x.shape[1])
+
+
+def _rope(grid, axes, theta, origin, pairing):
+    if pairing not in ("adjacent", "halves"):
+        raise ValueError('pairing is "adjacent" or "halves"')
+    g, a, o = _grid(grid), tuple(int(x) for x in axes), tuple(int(x) for x in origin)
+    if len(a) != 3 or len(o) != 3:
+        raise ValueError("axes and origin have three entries (time, height, width)")
+    return _lib.Rope(g, *o, *a, _lib.PAIRS_HALVES if pairing == "halves" else _lib.PAIRS_ADJACENT, float(theta))
+
+
+def _norm_weight(w, x, name):
+    torch = _torch()
+    if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (x.shape[3],) or not w.is_contiguous()
+                          or w.device != x.device):
+        raise ValueError("%s must be a contiguous float32 tensor [head_dim] on the queries' device" % name)
+    return w
+
+
+def _attention_layout(x, like, name):
+    """Checks a bf16 tensor in the attention's layout with the shape of `like`."""
+    torch = _torch()
+    if x.dtype != torch.bfloat16 or x.shape != like.shape or not x.is_contiguous() or x.device != like.device:
+        raise ValueError("%s must be a contiguous bfloat16 tensor %s on the queries' device" % (name, tuple(like.shape)))
+    return x
+
+
+def _type_of(x):
+    return _lib.TYPE_FP32 if x.dtype == _torch().float32 else _lib.TYPE_BF16
+
+
+def _tokens(grid):
+    f, h, w, nt = _grid_tuple(grid)
+    return f * h * w + nt
+
+
+def qk_norm_rope(q, k, grid, axes, q_weight=None, k_weight=None, norm=True, eps=1e-6, theta=10000.0,
+                 origin=(0, 0, 0), pairing="adjacent", q_out=None, k_out=None, stream=None):
+    """RMS norm of every head of the queries and keys, then the rotation by their (t, h, w) positions, into
+    the attention's layout (psa_qk_norm_rope_fwd).
+
+    q, k: bfloat16 or float32 [batch, heads, N, head_dim] of any strides with contiguous channels, such as
+    ``x.view(B, N, heads, d).transpose(1, 2)`` of a projection's output or a slice of a fused one (16-byte
+    aligned rows); k may have other heads than q, or be None.  Weights: float32 [head_dim], None for
+    ones; norm=False rotates alone.  axes: channels of the time, height and width axes; origin: position of
+    the first token (a later chunk of a clip).  Text tokens behind the video are not rotated.
+
+    Returns (q_out, k_out): bfloat16 [batch, heads, N, head_dim], contiguous."""
+    torch = _torch()
+    n = _tokens(grid)
+    rq = _rows(q, "q", q.dtype, n)
+    rk = _rows(k, "k", q.dtype, n, like=q) if k is not None else None
+    rope = _rope(grid, axes, theta, origin, pairing)
+    _norm_weight(q_weight, q, "q_weight")
+    _norm_weight(k_weight, q, "k_weight")
+    with torch.cuda.device(q.device), _on(stream):
+        yq = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if q_out is None else _attention_layout(q_out, q, "q_out")
+        yk = None
+        if k is not None:
+            yk = torch.empty(k.shape, dtype=torch.bfloat16, device=q.device) if k_out is None else _attention_layout(k_out, k, "k_out")
+        _lib.check(_lib.lib().psa_qk_norm_rope_fwd(
+            rq, rk, _ptr(yq), _ptr(yk), _type_of(q), q.shape[0], q.shape[3], rope, 1 if norm else 0, _ptr(q_weight),
+            _ptr(k_weight), float(eps), _stream(None, q.device)))
+    return yq, yk
+
+
+def _empty_rows(x):
+    """Uninitialised rows in the order of x (a dense tensor where x is a slice or repeats rows)."""
+    torch = _torch()
+    if any(s == 0 and size > 1 for s, size in zip(x.stride(), x.shape)):
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    return torch.empty_like(x)
+
+
+def qk_norm_rope_bwd(dq_out, dk_out, q, k, grid, axes, q_weight=None, k_weight=None, norm=True, eps=1e-6,
+                     theta=10000.0, origin=(0, 0, 0), pairing="adjacent", dq=None, dk=None, workspace=None,
+                     stream=None):
+    """Gradients of qk_norm_rope (psa_qk_norm_rope_bwd): dq_out and dk_out are those of its outputs (bfloat16,
+    contiguous), the other arguments the forward's.
+
+    Returns (dq, dk, dq_weight, dk_weight): dq and dk in the type and order of q and k (or in the tensors
+    given, of any strides as for q and k: a fused projection's gradient), one row for each row of the outputs,
+    also where an input repeats rows; the weights' float32 [head_dim], None without a norm."""
+    torch = _torch()
+    n = _tokens(grid)
+    rq = _rows(q, "q", q.dtype, n)
+    rk = _rows(k, "k", q.dtype, n, like=q) if k is not None else None
+    rope = _rope(grid, axes, theta, origin, pairing)
+    _norm_weight(q_weight, q, "q_weight")
+    _norm_weight(k_weight, q, "k_weight")
+    _attention_layout(dq_out, q, "dq_out")
+    if k is not None:
+        _attention_layout(dk_out, k, "dk_out")
+    with torch.cuda.device(q.device), _on(stream):
+        grads, rows = [], []
+        for given, x, name in ((dq, q, "dq"), (dk, k, "dk")):
+            if x is None:
+                grads.append(None)
+                rows.append(None)
+                continue
+            g = _empty_rows(x) if given is None else given
+            if g.shape != x.shape:
+                raise ValueError("%s must have the shape %s" % (name, tuple(x.shape)))
+            grads.append(g)
+            rows.append(_rows(g, name, q.dtype, n, like=q))
+        dw = [torch.empty(q.shape[3], dtype=torch.float32, device=q.device) if norm and x is not None else None
+              for x in (q, k)]
+        nbytes = int(_lib.lib().psa_qk_norm_rope_workspace_size(
+            q.shape[0], q.shape[1], k.shape[1] if k is not None else 0, q.shape[3], _grid(grid), 1 if norm else 0))
+        if workspace is None and nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        _lib.check(_lib.lib().psa_qk_norm_rope_bwd(
+            _ptr(dq_out), _ptr(dk_out) if k is not None else None, rq, rk, rows[0], rows[1], _ptr(dw[0]), _ptr(dw[1]),
+            _type_of(q), q.shape[0], q.shape[3], rope, 1 if norm else 0, _ptr(q_weight), _ptr(k_weight), float(eps),
+            _ptr(workspace), ws_bytes, _stream(None, q.device)))
+    return grads[0], grads[1], dw[0], dw[1]

@@ -19,6 +19,9 @@ MAX_BLOCKS = 7936
 MAX_BATCH_HEADS = 1024
 NOALLOC_SCRATCH_BYTES = 16 << 20
 
+TYPE_BF16, TYPE_FP32 = 0, 1
+PAIRS_ADJACENT, PAIRS_HALVES = 0, 1
+
 PSA_OK = 0
 PSA_ERR_INVALID = 1
 PSA_ERR_UNSUPPORTED = 2
@@ -30,6 +33,7 @@ EXPORTS = ("psa_num_blocks", "psa_workspace_size", "psa_build_blockmap", "psa_at
            "psa_blocked_tokens",
            "psa_to_blocks", "psa_from_blocks", "psa_build_blockmap_3d", "psa_workspace_size_3d",
            "psa_attention_plan_3d", "psa_attention_run_3d", "psa_l2_workspace_size", "psa_l2_distance",
+           "psa_qk_norm_rope_fwd", "psa_qk_norm_rope_workspace_size", "psa_qk_norm_rope_bwd",
            "psa_status_string", "psa_last_error")
 
 
@@ -45,6 +49,17 @@ class Grid(ctypes.Structure):
 
 class Block3d(ctypes.Structure):
     _fields_ = [("t", ctypes.c_int32), ("h", ctypes.c_int32), ("w", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_n", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("grid", Grid), ("origin_t", ctypes.c_int32), ("origin_h", ctypes.c_int32),
+                ("origin_w", ctypes.c_int32), ("axis_t", ctypes.c_int32), ("axis_h", ctypes.c_int32),
+                ("axis_w", ctypes.c_int32), ("pairs", ctypes.c_int32), ("theta", ctypes.c_double)]
 
 
 class PsaError(RuntimeError):
@@ -117,6 +132,14 @@ def lib():
         L.psa_l2_workspace_size.restype = sz
         L.psa_l2_distance.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
         L.psa_l2_distance.restype = ctypes.c_int
+        rows, rope = ctypes.POINTER(Rows), ctypes.POINTER(Rope)
+        L.psa_qk_norm_rope_fwd.argtypes = [rows, rows, vp, vp, i32, i32, i32, rope, i32, vp, vp, ctypes.c_float, vp]
+        L.psa_qk_norm_rope_fwd.restype = ctypes.c_int
+        L.psa_qk_norm_rope_workspace_size.argtypes = [i32, i32, i32, i32, Grid, i32]
+        L.psa_qk_norm_rope_workspace_size.restype = sz
+        L.psa_qk_norm_rope_bwd.argtypes = [vp, vp, rows, rows, rows, rows, vp, vp, i32, i32, i32, rope, i32, vp, vp,
+                                           ctypes.c_float, vp, sz, vp]
+        L.psa_qk_norm_rope_bwd.restype = ctypes.c_int
         L.psa_status_string.argtypes = [ctypes.c_int]
         L.psa_status_string.restype = ctypes.c_char_p
         L.psa_last_error.argtypes = []

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "psa_launch.h"
 
@@ -259,6 +260,81 @@ psa_status_t run_planned(const void* q, const void* k, const void* v, void* o, i
                                     params ? (int32_t)psa::plan_full(g, params, n_heads) : -1);
   if (e != hipSuccess) return hip_fail(e, "psa_attention_run kernel launch");
   return PSA_OK;
+}
+
+// One tensor of a norm-and-rotation call.  write: the rows are an output.
+psa_status_t check_rows(const psa_rows_t& r, const char* what, int32_t batch, int64_t n, int32_t type, bool write) {
+  const int64_t unit = type == PSA_TYPE_BF16 ? 8 : 4;       // elements of 16 bytes
+  if (!r.x) return fail(PSA_ERR_INVALID, "%s is NULL", what);
+  if (!aligned(r.x, 16)) return fail(PSA_ERR_INVALID, "%s must be 16-byte aligned (%p)", what, r.x);
+  if (r.n_heads < 1) return fail(PSA_ERR_INVALID, "%s: n_heads must be >= 1 (got %d)", what, r.n_heads);
+  if (r.stride_b % unit || r.stride_h % unit || r.stride_n % unit || r.stride_b < 0 || r.stride_h < 0 || r.stride_n < 0)
+    return fail(PSA_ERR_INVALID, "%s: strides must be multiples of 16 bytes, not negative (%lld, %lld, %lld)", what,
+                (long long)r.stride_b, (long long)r.stride_h, (long long)r.stride_n);
+  if (write && ((batch > 1 && !r.stride_b) || (r.n_heads > 1 && !r.stride_h) || (n > 1 && !r.stride_n)))
+    return fail(PSA_ERR_INVALID, "%s: an output's rows must not share memory", what);
+  return PSA_OK;
+}
+
+// Shapes and the rotation of a norm-and-rotation call; fills all of `a` but its tensors.
+psa_status_t check_rope(int32_t type, int32_t batch, int32_t n_tensors, int32_t head_dim, const psa_rope_t* rope,
+                        int32_t norm, const float* q_weight, const float* k_weight, float eps, psa::RopeArgs* a) {
+  if (type != PSA_TYPE_BF16 && type != PSA_TYPE_FP32)
+    return fail(PSA_ERR_UNSUPPORTED, "type must be PSA_TYPE_BF16 or PSA_TYPE_FP32 (got %d)", type);
+  if (batch < 1) return fail(PSA_ERR_INVALID, "batch must be >= 1 (got %d)", batch);
+  if ((int64_t)batch * n_tensors > 65535) return fail(PSA_ERR_UNSUPPORTED, "batch %d is too large", batch);
+  if (head_dim != 64 && head_dim != 128)
+    return fail(PSA_ERR_UNSUPPORTED, "head_dim must be 64 or 128 (got %d)", head_dim);
+  if (!rope) return fail(PSA_ERR_INVALID, "rope is NULL");
+  psa::Geometry g;
+  if (!grid_geometry(rope->grid, 1, &g))
+    return fail(PSA_ERR_INVALID, "invalid grid (%d x %d x %d + %d text)", rope->grid.frames, rope->grid.height,
+                rope->grid.width, rope->grid.n_text);
+  const int32_t axes[3] = {rope->axis_t, rope->axis_h, rope->axis_w};
+  const int32_t origin[3] = {rope->origin_t, rope->origin_h, rope->origin_w};
+  const int32_t extent[3] = {rope->grid.frames, rope->grid.height, rope->grid.width};
+  int64_t channels = 0;
+  for (int i = 0; i < 3; i++) {
+    if (axes[i] < 0 || axes[i] % 2) return fail(PSA_ERR_INVALID, "channels of an axis must be even and >= 0 (got %d)", axes[i]);
+    if ((int64_t)origin[i] + extent[i] > INT32_MAX) return fail(PSA_ERR_INVALID, "positions from %d on are too large", origin[i]);
+    channels += axes[i];
+  }
+  if (channels > head_dim) return fail(PSA_ERR_INVALID, "the axes have %lld channels, a head %d", (long long)channels, head_dim);
+  if (rope->pairs != PSA_PAIRS_ADJACENT && rope->pairs != PSA_PAIRS_HALVES)
+    return fail(PSA_ERR_INVALID, "pairs must be PSA_PAIRS_ADJACENT or PSA_PAIRS_HALVES (got %d)", rope->pairs);
+  if (rope->pairs == PSA_PAIRS_HALVES && channels != head_dim)
+    return fail(PSA_ERR_INVALID, "pairs across the halves need axes that fill the head (%lld of %d channels)",
+                (long long)channels, head_dim);
+  if (!(rope->theta > 0) || !std::isfinite(rope->theta)) return fail(PSA_ERR_INVALID, "theta must be positive and finite");
+  if (!(eps >= 0) || !std::isfinite(eps)) return fail(PSA_ERR_INVALID, "eps must be >= 0 and finite");
+  if (!norm && (q_weight || k_weight)) return fail(PSA_ERR_INVALID, "weights without a norm");
+  if (!aligned(q_weight, 4) || !aligned(k_weight, 4)) return fail(PSA_ERR_INVALID, "weights must be 4-byte aligned");
+  *a = psa::RopeArgs{};
+  a->n_tensors = n_tensors;
+  a->batch = batch;
+  a->n = g.n;
+  a->n_video = g.n_video;
+  a->hw = g.hw;
+  a->width = rope->grid.width;
+  a->eps = eps;
+  a->t[0].weight = q_weight;
+  a->t[1].weight = k_weight;
+  int pair = 0;
+  for (int i = 0; i < 3; i++) {
+    a->origin[i] = origin[i];
+    for (int j = 0; j < axes[i] / 2; j++)
+      a->turns[pair++] = std::pow(rope->theta, -2.0 * j / axes[i]) * 0.15915494309189533577;    // 1 / (2 pi)
+    if (i < 2) a->end[i] = pair;
+  }
+  return PSA_OK;
+}
+
+void set_rows(psa::RopeTensor* t, const psa_rows_t& r) {
+  t->x = r.x;
+  t->stride_b = r.stride_b;
+  t->stride_h = r.stride_h;
+  t->stride_n = r.stride_n;
+  t->n_heads = r.n_heads;
 }
 
 }  // namespace
@@ -516,6 +592,86 @@ psa_status_t psa_l2_distance(const void* o, const void* ref, int32_t batch_heads
   hipError_t e = psa::launch_l2(o, ref, batch_heads, (int64_t)n_tokens * head_dim, (double*)workspace,
                                 sq_err, sq_ref, stream);
   return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_l2_distance launch");
+}
+
+psa_status_t psa_qk_norm_rope_fwd(const psa_rows_t* q, const psa_rows_t* k, void* q_out, void* k_out,
+                                  int32_t type, int32_t batch, int32_t head_dim, const psa_rope_t* rope,
+                                  int32_t norm, const float* q_weight, const float* k_weight, float eps,
+                                  hipStream_t stream) {
+  psa::RopeArgs a;
+  psa_status_t s = check_rope(type, batch, k ? 2 : 1, head_dim, rope, norm, q_weight, k_weight, eps, &a);
+  if (s != PSA_OK) return s;
+  if (!q) return fail(PSA_ERR_INVALID, "q is NULL");
+  const psa_rows_t* rows[2] = {q, k};
+  void* out[2] = {q_out, k_out};
+  for (int i = 0; i < a.n_tensors; i++) {
+    s = check_rows(*rows[i], i ? "k" : "q", batch, a.n, type, false);
+    if (s != PSA_OK) return s;
+    if (!out[i] || !aligned(out[i], 16))
+      return fail(PSA_ERR_INVALID, "outputs must be non-NULL and 16-byte aligned (%p)", out[i]);
+    set_rows(&a.t[i], *rows[i]);
+    a.t[i].y = out[i];
+  }
+  const hipError_t e = psa::launch_norm_rope(a, head_dim, type == PSA_TYPE_FP32, norm, rope->pairs == PSA_PAIRS_HALVES, stream);
+  return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_qk_norm_rope_fwd launch");
+}
+
+size_t psa_qk_norm_rope_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, psa_grid_t grid, int32_t norm) {
+  psa::Geometry g;
+  if (!norm || batch < 1 || n_heads < 1 || n_kv_heads < 0 || (head_dim != 64 && head_dim != 128) ||
+      (int64_t)batch * 2 > 65535 || !grid_geometry(grid, 1, &g))
+    return 0;
+  psa::RopeArgs a = {};
+  a.batch = batch;
+  a.n = g.n;
+  a.n_tensors = n_kv_heads > 0 ? 2 : 1;
+  a.t[0].n_heads = n_heads;
+  a.t[1].n_heads = n_kv_heads;
+  return (size_t)(psa::rope_partial_rows(a, head_dim) * a.n_tensors * head_dim) * sizeof(float);
+}
+
+psa_status_t psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const psa_rows_t* q,
+                                  const psa_rows_t* k, const psa_rows_t* dq, const psa_rows_t* dk,
+                                  float* dq_weight, float* dk_weight, int32_t type, int32_t batch,
+                                  int32_t head_dim, const psa_rope_t* rope, int32_t norm,
+                                  const float* q_weight, const float* k_weight, float eps, void* workspace,
+                                  size_t workspace_bytes, hipStream_t stream) {
+  psa::RopeArgs a;
+  psa_status_t s = check_rope(type, batch, k ? 2 : 1, head_dim, rope, norm, q_weight, k_weight, eps, &a);
+  if (s != PSA_OK) return s;
+  if (!q || !dq || (k && !dk)) return fail(PSA_ERR_INVALID, "q, dq and, with k, dk must be non-NULL");
+  const psa_rows_t *rows[2] = {q, k}, *grads[2] = {dq, dk};
+  const void* dy[2] = {dq_out, dk_out};
+  float* dw[2] = {dq_weight, dk_weight};
+  for (int i = 0; i < a.n_tensors; i++) {
+    if (norm) {
+      s = check_rows(*rows[i], i ? "k" : "q", batch, a.n, type, false);
+      if (s != PSA_OK) return s;
+      if (!dw[i] || !aligned(dw[i], 4))
+        return fail(PSA_ERR_INVALID, "the weights' gradients must be non-NULL and 4-byte aligned (%p)", (void*)dw[i]);
+    }
+    s = check_rows(*grads[i], i ? "dk" : "dq", batch, a.n, type, true);
+    if (s != PSA_OK) return s;
+    if (grads[i]->n_heads != rows[i]->n_heads)
+      return fail(PSA_ERR_INVALID, "gradients of %d heads for %d", grads[i]->n_heads, rows[i]->n_heads);
+    if (!dy[i] || !aligned(dy[i], 16))
+      return fail(PSA_ERR_INVALID, "dq_out and dk_out must be non-NULL and 16-byte aligned (%p)", dy[i]);
+    set_rows(&a.t[i], *rows[i]);
+    a.t[i].dy = dy[i];
+    a.t[i].dx = grads[i]->x;
+    a.t[i].dx_stride_b = grads[i]->stride_b;
+    a.t[i].dx_stride_h = grads[i]->stride_h;
+    a.t[i].dx_stride_n = grads[i]->stride_n;
+  }
+  const size_t need = psa_qk_norm_rope_workspace_size(batch, q->n_heads, k ? k->n_heads : 0, head_dim, rope->grid, norm);
+  if (norm && (!workspace || workspace_bytes < need))
+    return fail(PSA_ERR_WORKSPACE, "workspace of %zu bytes at %p; %zu bytes required", workspace_bytes, workspace, need);
+  if (!aligned(workspace, 256)) return fail(PSA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  a.partial = (float*)workspace;
+  const hipError_t e = psa::launch_norm_rope_bwd(a, head_dim, type == PSA_TYPE_FP32, norm,
+                                                 rope->pairs == PSA_PAIRS_HALVES, dq_weight, dk_weight, stream);
+  return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_qk_norm_rope_bwd launch");
 }
 
 const char* psa_status_string(psa_status_t status) {

@@ -226,6 +226,41 @@ hipError_t launch_dense(const void* q, const void* k, const void* v, void* o, fl
                         int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_tokens,
                         int32_t block, float scale_log2, int32_t* queues, int32_t cus, hipStream_t stream);
 
+// One tensor of a norm-and-rotation launch: rows of head_dim channels by strides in elements.
+struct RopeTensor {
+  const void* x;              // bf16 or fp32; backward without a norm: unused
+  int64_t stride_b, stride_h, stride_n;
+  const float* weight;        // [head_dim], null: ones
+  void* y;                    // forward: bf16 [batch][n_heads][n][head_dim]
+  const void* dy;             // backward: the gradient of y
+  void* dx;                   // backward: in the type of x, by strides of its own
+  int64_t dx_stride_b, dx_stride_h, dx_stride_n;
+  int32_t n_heads;
+};
+
+constexpr int kRopePairs = 64;  // channel pairs of the largest head
+
+struct RopeArgs {
+  RopeTensor t[2];
+  int32_t n_tensors, batch;
+  int32_t n, n_video, hw, width;      // tokens, those of the video, those of a frame, those of a line
+  int32_t origin[3];                  // position (t, h, w) of the first token
+  int32_t end[2];                     // pairs below end[0] turn by t, below end[1] by h, the others by w
+  float eps;
+  float* partial;                     // backward with a norm: partial sums of the weights' gradients
+  int32_t wide, tiles, heads_per_group;   // set by the launcher
+  double turns[kRopePairs];           // turns per position of every pair, theta^(-2 j / d_a) / (2 pi)
+};
+
+// Rows of partial sums per tensor that the backward of these sizes writes.
+int64_t rope_partial_rows(RopeArgs args, int32_t head_dim);
+
+hipError_t launch_norm_rope(const RopeArgs& args, int32_t head_dim, bool f32, bool norm, bool halves,
+                            hipStream_t stream);
+// dq_weight, dk_weight: fp32 [head_dim], written where there is a norm.
+hipError_t launch_norm_rope_bwd(const RopeArgs& args, int32_t head_dim, bool f32, bool norm, bool halves,
+                                float* dq_weight, float* dk_weight, hipStream_t stream);
+
 // Device address of the static scratch of psa_attention_fwd_noalloc on the current device
 // (PSA_NOALLOC_SCRATCH_BYTES, 256-byte aligned), looked up once per device.
 hipError_t scratch_pointer(void** out);

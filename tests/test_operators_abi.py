@@ -1,0 +1,62 @@
+"""Refusals of the operators around the attention at the C ABI, on the CPU: invalid arguments are rejected
+with the documented status codes before the GPU is touched."""
+import ctypes
+
+import pytest
+
+from paper_2609_37001_amd import _lib
+
+vp = lambda x: ctypes.c_void_p(x) if x else None
+INVALID, UNSUPPORTED, WORKSPACE = _lib.PSA_ERR_INVALID, _lib.PSA_ERR_UNSUPPORTED, _lib.PSA_ERR_WORKSPACE
+
+
+def rows(x=256, b=4096, h=512, n=64, heads=2):
+    return _lib.Rows(x, b, h, n, heads)
+
+
+def rope(grid=(1, 2, 3, 1), origin=(0, 0, 0), axes=(24, 20, 20), pairs=0, theta=1e4):
+    return _lib.Rope(_lib.grid_of(*grid), *origin, *axes, pairs, theta)
+
+
+def fwd(q=rows(), k=rows(), qo=256, ko=256, dtype=0, batch=1, d=64, r=rope(), norm=1, qw=0, kw=0, eps=1e-6):
+    return _lib.lib().psa_qk_norm_rope_fwd(q, k, vp(qo), vp(ko), dtype, batch, d, r, norm, vp(qw), vp(kw), eps, None)
+
+
+@pytest.mark.parametrize("status,bad", [
+    (INVALID, dict(q=None)), (INVALID, dict(q=rows(x=0))), (INVALID, dict(q=rows(x=264))), (INVALID, dict(k=rows(x=8))),
+    (INVALID, dict(qo=0)), (INVALID, dict(ko=8)), (INVALID, dict(q=rows(n=68))), (INVALID, dict(q=rows(h=-64))),
+    (INVALID, dict(q=rows(b=4))), (INVALID, dict(q=rows(heads=0))), (UNSUPPORTED, dict(dtype=2)),
+    (INVALID, dict(batch=0)), (UNSUPPORTED, dict(batch=40000)), (UNSUPPORTED, dict(d=96)), (INVALID, dict(r=None)),
+    (INVALID, dict(r=rope(grid=(0, 2, 3, 1)))), (INVALID, dict(r=rope(grid=(1, 2, 3, -1)))),
+    (INVALID, dict(r=rope(axes=(25, 20, 19)))), (INVALID, dict(r=rope(axes=(-2, 20, 20)))),
+    (INVALID, dict(r=rope(axes=(44, 42, 42)))), (INVALID, dict(r=rope(pairs=2))),
+    (INVALID, dict(r=rope(axes=(24, 20, 0), pairs=1))), (INVALID, dict(r=rope(theta=0.0))),
+    (INVALID, dict(r=rope(theta=float("nan")))), (INVALID, dict(r=rope(theta=float("inf")))),
+    (INVALID, dict(r=rope(origin=(2 ** 31 - 1, 0, 0)))), (INVALID, dict(eps=-1.0)), (INVALID, dict(eps=float("nan"))),
+    (INVALID, dict(norm=0, qw=256)), (INVALID, dict(qw=258)), (INVALID, dict(kw=3)),
+    (INVALID, dict(dtype=1, q=rows(n=66)))])
+def test_norm_rope_refusals(status, bad):
+    assert fwd(**bad) == status
+    assert _lib.lib().psa_last_error()
+
+
+def bwd(dqo=256, dko=256, q=rows(), k=rows(), dq=rows(), dk=rows(), dqw=256, dkw=256, norm=1, ws=256, wsb=1 << 24):
+    return _lib.lib().psa_qk_norm_rope_bwd(vp(dqo), vp(dko), q, k, dq, dk, vp(dqw), vp(dkw), 0, 1, 64, rope(), norm,
+                                           None, None, 1e-6, vp(ws), wsb, None)
+
+
+@pytest.mark.parametrize("status,bad", [
+    (INVALID, dict(q=None)), (INVALID, dict(dq=None)), (INVALID, dict(dk=None)), (INVALID, dict(dqo=0)),
+    (INVALID, dict(dko=8)), (INVALID, dict(q=rows(x=0))), (INVALID, dict(dq=rows(h=0))), (INVALID, dict(dk=rows(n=0))),
+    (INVALID, dict(dq=rows(heads=3))), (INVALID, dict(dqw=0)), (INVALID, dict(dkw=2)), (WORKSPACE, dict(ws=0)),
+    (WORKSPACE, dict(ws=128)), (WORKSPACE, dict(wsb=8)), (INVALID, dict(norm=0, q=rows(x=0), dq=rows(x=4)))])
+def test_norm_rope_bwd_refusals(status, bad):
+    assert bwd(**bad) == status
+
+
+def test_norm_rope_workspace_size():
+    size = lambda *a: _lib.lib().psa_qk_norm_rope_workspace_size(*a)
+    g = _lib.grid_of(21, 30, 52)
+    assert size(1, 12, 12, 128, g, 1) >= 2 * 128 * 4 and size(1, 12, 0, 128, g, 1) > 0
+    assert size(1, 12, 12, 128, g, 0) == size(0, 12, 12, 128, g, 1) == size(1, 0, 1, 128, g, 1) == 0
+    assert size(1, 12, 12, 96, g, 1) == size(1, 12, 12, 64, _lib.grid_of(0, 1, 1), 1) == 0
