@@ -375,6 +375,83 @@ psa_status_t psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const 
                                   const float* q_weight, const float* k_weight, float eps, void* workspace,
                                   size_t workspace_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Block selection, and attention over any block map.  A map holds a byte for every (query block, key
+ * block) of every query head, not 0 where the tile is kept: psa_build_blockmap's maps, those of
+ * psa_select_blocks, or a caller's own.  Queries and keys may have different lengths (a few new rows over a
+ * long cache, down to one) and a key head may serve several
+ * consecutive query heads.
+ * Blocks are runs of `block` tokens from the first on, the last of each side partial.
+ * --------------------------------------------------------------------------------------------- */
+
+/* Keys and values, bf16 [batch][n_heads][n_k][head_dim]: rows contiguous, batch elements and heads by strides in
+ * elements (a part of a longer cache; multiples of 8, 0 repeats), 16-byte aligned. */
+typedef struct {
+  const void* k;
+  const void* v;              /* psa_select_blocks does not read it */
+  int64_t stride_b, stride_h;
+  int32_t n_heads;            /* divides the queries' n_heads */
+} psa_kv_t;
+
+/* Bytes of device workspace of psa_select_blocks (0 if invalid). */
+size_t psa_select_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t n_q, int32_t n_k, int32_t block);
+
+/* The key blocks that a cheap score selects for each query block: the score of a pair is the inner product of the
+ * means of the block's queries and of the block's keys.  A row keeps the `keep` highest-scoring key blocks that
+ * hold no text (all of them if there are fewer; of equal scores the lowest index first, NaN lowest) and every
+ * key block that holds any of the last k_text keys; a query block that holds any of the last q_text queries
+ * keeps every key block.  Means and scores are in 64 bits.
+ *   q             device bf16 [batch][n_heads][n_q][head_dim], 16-byte aligned
+ *   blockmap      device uint8 [batch][n_heads][nbq][nbk], nb = ceil(n / block): 0 or 1
+ *   kept_per_row  device int32 [batch][n_heads][nbq], or NULL
+ *   workspace     device, psa_select_workspace_size() bytes, 256-byte aligned
+ * head_dim and block 64 or 128; at most PSA_MAX_BLOCKS blocks on each side. */
+psa_status_t psa_select_blocks(const void* q, const psa_kv_t* kv, int32_t batch, int32_t n_heads,
+                               int32_t head_dim, int32_t n_q, int32_t n_k, int32_t block, int32_t keep,
+                               int32_t q_text, int32_t k_text, uint8_t* blockmap, int32_t* kept_per_row,
+                               void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of device workspace of psa_attention_map_fwd (0 if invalid, or if none is needed: only calls of few
+ * query blocks, whose lists are shared out over several workgroups, need one). */
+size_t psa_attention_map_workspace_size(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_q,
+                                        int32_t n_k, int32_t block);
+
+/* Attention over a block map: o = softmax(scale * q k^T restricted to the kept tiles) v, numerics and empty rows
+ * as psa_attention_fwd.
+ *   q, o         device bf16 [batch][n_heads][n_q][head_dim], 16-byte aligned
+ *   blockmap     device uint8 [n_heads][nbq][nbk] per batch element, map_stride_b bytes from one to the next
+ *                (0: the same map for all)
+ *   lse          device fp32 [batch][n_heads][n_q], or NULL
+ *   workspace    device, psa_attention_map_workspace_size() bytes, 256-byte aligned (NULL if 0)
+ * head_dim and block 64 or 128; at most PSA_MAX_BLOCKS blocks on each side. */
+psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, int32_t batch,
+                                   int32_t n_heads, int32_t head_dim, int32_t n_q, int32_t n_k,
+                                   int32_t block, const uint8_t* blockmap, int64_t map_stride_b,
+                                   float softmax_scale, float* lse, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of device workspace of psa_attention_map_bwd (0 if invalid). */
+size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_q,
+                                            int32_t block);
+
+/* Gradients of psa_attention_map_fwd.  Scores are formed again as the forward does (q scaled and rounded to bf16
+ * once, also in dk; products summed in fp32), so that the weights are those of its lse; the weights and their
+ * gradients are rounded to bf16 before the products that sum them, which are in fp32; dq, dk and dv are
+ * rounded to bf16 once.  A shared key head's gradients are the sums over its query heads.
+ * The order of every sum is fixed by the call's sizes and map.
+ *   grad_o, o    device bf16 [batch][n_heads][n_q][head_dim]; o and lse as the forward left them
+ *   dq           device bf16 [batch][n_heads][n_q][head_dim]: 0 for rows that keep nothing
+ *   dk, dv       device bf16 [batch][kv->n_heads][n_k][head_dim], contiguous: 0 for keys that no row keeps
+ *   workspace    device, psa_attention_map_bwd_workspace_size() bytes, 256-byte aligned
+ * Tensors 16-byte aligned; the outputs must not overlap any input or each other. */
+psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_kv_t* kv, const void* o,
+                                   const float* lse, int32_t batch, int32_t n_heads, int32_t head_dim,
+                                   int32_t n_q, int32_t n_k, int32_t block, const uint8_t* blockmap,
+                                   int64_t map_stride_b, float softmax_scale, void* dq, void* dk,
+                                   void* dv, void* workspace, size_t workspace_bytes,
+                                   hipStream_t stream);
+
 /* Static description of a status code. */
 const char* psa_status_string(psa_status_t status);
 

@@ -22,6 +22,12 @@ is no CPU or PyTorch fallback.
 Norms and 3D rotary positions of queries and keys, from the projection's [batch, N, heads, d]:
 
     q, k = qk_norm_rope(xq.transpose(1, 2), xk.transpose(1, 2), grid, (44, 42, 42), q_weight=wq, k_weight=wk)
+
+Attention over a map of blocks that a score of the data selects (or over any other block map):
+
+    bmap, kept = select_blocks(q, k, block=128, keep=64)
+    o, lse = attention_map_fwd(q, k, v, bmap, block=128, return_lse=True)
+    dq, dk, dv = attention_map_bwd(do, q, k, v, o, lse, bmap, block=128)
 """
 import contextlib
 import math
@@ -32,7 +38,8 @@ from ._lib import STRIDE_INF, PsaError  # noqa: F401
 __all__ = ["STRIDE_INF", "PsaError", "num_blocks", "workspace_size", "build_blockmap",
            "attention_fwd", "attention_fwd_noalloc", "plan", "run", "dense_fwd", "dense_workspace_size", "Workspace", "library_path",
            "blocked_tokens", "to_blocks", "from_blocks", "build_blockmap_3d", "plan_3d", "run_3d",
-           "attention_fwd_3d", "l2_distance", "qk_norm_rope", "qk_norm_rope_bwd"]
+           "attention_fwd_3d", "l2_distance", "qk_norm_rope", "qk_norm_rope_bwd", "select_blocks",
+           "attention_map_fwd", "attention_map_bwd"]
 
 
 def library_path():
@@ -563,11 +570,156 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, grid, axes, q_weight=None, k_weight=N
               for x in (q, k)]
         nbytes = int(_lib.lib().psa_qk_norm_rope_workspace_size(
             q.shape[0], q.shape[1], k.shape[1] if k is not None else 0, q.shape[3], _grid(grid), 1 if norm else 0))
-        if workspace is None and nbytes:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        ws, ws_bytes, _keep = _workspace(workspace, nbytes, q.device)
         _lib.check(_lib.lib().psa_qk_norm_rope_bwd(
             _ptr(dq_out), _ptr(dk_out) if k is not None else None, rq, rk, rows[0], rows[1], _ptr(dw[0]), _ptr(dw[1]),
             _type_of(q), q.shape[0], q.shape[3], rope, 1 if norm else 0, _ptr(q_weight), _ptr(k_weight), float(eps),
-            _ptr(workspace), ws_bytes, _stream(None, q.device)))
+            ws, ws_bytes, _stream(None, q.device)))
     return grads[0], grads[1], dw[0], dw[1]
+
+
+# ---------------------------------------------------------------------------------------------
+# Block selection, and attention over any block map (include/psa.h, fifth part).
+# ---------------------------------------------------------------------------------------------
+
+def _check_q(q, name="q", like=None):
+    torch = _torch()
+    if q.dtype != torch.bfloat16:
+        raise TypeError("%s must be bfloat16" % name)
+    if not q.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    if q.dim() != 4 or not q.is_contiguous():
+        raise ValueError("%s must be contiguous [batch, heads, N, head_dim]" % name)
+    if like is not None and (q.shape != like.shape or q.device != like.device):
+        raise ValueError("%s must have the shape %s, on the queries' device" % (name, tuple(like.shape)))
+
+
+def _kv(q, k, v=None):
+    """psa_kv_t of keys and values: [batch, kv heads, N_k, head_dim], each head's rows contiguous."""
+    torch = _torch()
+    for t in (k,) if v is None else (k, v):
+        if t.dtype != torch.bfloat16:
+            raise TypeError("k and v must be bfloat16")
+        if t.device != q.device:
+            raise ValueError("k and v must be on the queries' device")
+        if t.dim() != 4 or t.shape[0] != q.shape[0] or t.shape[3] != q.shape[3]:
+            raise ValueError("k and v must be [batch, kv heads, N_k, head_dim] with the queries' batch and head_dim")
+        if t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != t.shape[3]):
+            raise ValueError("the rows of a head of k and v must be contiguous")
+    strides = [s if size > 1 else 0 for s, size in zip(k.stride()[:2], k.shape)]
+    if v is not None and (v.shape != k.shape or [s if size > 1 else 0 for s, size in zip(v.stride()[:2], v.shape)] != strides):
+        raise ValueError("k and v must share their shape and strides")
+    return _lib.Kv(k.data_ptr(), _ptr(v), *strides, k.shape[1])
+
+
+def _blocks(n, block):
+    return -(-n // int(block)) if int(block) > 0 else 0
+
+
+def _map_of(blockmap, q, n_k, block):
+    """(pointer, bytes between batch elements) of a map [batch, heads, nbq, nbk] or [heads, nbq, nbk]."""
+    torch = _torch()
+    if blockmap.dtype not in (torch.uint8, torch.bool):
+        raise TypeError("blockmap must be uint8 or bool")
+    shape = (q.shape[1], _blocks(q.shape[2], block), _blocks(n_k, block))
+    if blockmap.device != q.device or tuple(blockmap.shape) not in (shape, (q.shape[0],) + shape):
+        raise ValueError("blockmap must be %s or %s on the queries' device" % (shape, (q.shape[0],) + shape))
+    one = blockmap if blockmap.dim() == 3 else blockmap[0]
+    if not one.is_contiguous():
+        raise ValueError("the maps of a batch element must be contiguous")
+    return blockmap.data_ptr(), blockmap.stride(0) if blockmap.dim() == 4 and q.shape[0] > 1 else 0
+
+
+def _workspace(workspace, nbytes, device):
+    """(pointer, bytes) of a workspace tensor, a fresh one if none is given and one is needed; and that tensor, which
+    has to live until the call has been enqueued."""
+    torch = _torch()
+    if workspace is None and nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if workspace is None:
+        return None, 0, None
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("the workspace must be a contiguous tensor on the queries' device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def select_blocks(q, k, block, keep, q_text=0, k_text=0, blockmap=None, workspace=None, stream=None):
+    """For every query block the `keep` key blocks of the highest mean score, with the text's (psa_select_blocks).
+
+    q: bfloat16 [batch, heads, N_q, head_dim], contiguous; k: [batch, kv heads, N_k, head_dim], each head's rows
+    contiguous (kv heads divide heads); q_text, k_text: text tokens at the end of each.
+
+    Returns (map uint8 [batch, heads, nbq, nbk], kept_per_row int32 [batch, heads, nbq])."""
+    torch = _torch()
+    _check_q(q)
+    kv = _kv(q, k)
+    b, h, n_q, d = q.shape
+    n_k = k.shape[2]
+    shape = (b, h, _blocks(n_q, block), _blocks(n_k, block))
+    with torch.cuda.device(q.device), _on(stream):
+        m = torch.empty(shape, dtype=torch.uint8, device=q.device) if blockmap is None else blockmap
+        if tuple(m.shape) != shape or m.dtype != torch.uint8 or not m.is_contiguous() or m.device != q.device:
+            raise ValueError("blockmap must be a contiguous uint8 tensor %s on the queries' device" % (shape,))
+        kept = torch.empty(shape[:3], dtype=torch.int32, device=q.device)
+        L = _lib.lib()
+        ws, nbytes, _keep = _workspace(workspace, int(L.psa_select_workspace_size(b, h, k.shape[1], d, n_q, n_k, int(block))), q.device)
+        _lib.check(L.psa_select_blocks(_ptr(q), kv, b, h, d, n_q, n_k, int(block), int(keep), int(q_text), int(k_text),
+                                       _ptr(m), _ptr(kept), ws, nbytes, _stream(None, q.device)))
+    return m, kept
+
+
+def attention_map_fwd(q, k, v, blockmap, block, scale=None, out=None, return_lse=False, workspace=None, stream=None):
+    """Attention over the kept tiles of a block map (psa_attention_map_fwd).
+
+    q: bfloat16 [batch, heads, N_q, head_dim], contiguous; k, v: [batch, kv heads, N_k, head_dim] with the same
+    strides, each head's rows contiguous (a part of a longer cache; kv heads divide heads); blockmap: uint8 or bool
+    [batch, heads, nbq, nbk], or [heads, nbq, nbk] for every batch element (build_blockmap's, select_blocks').
+
+    Returns o like q (and lse float32 [batch, heads, N_q] if asked)."""
+    torch = _torch()
+    _check_q(q)
+    kv = _kv(q, k, v)
+    b, h, n_q, d = q.shape
+    n_k = k.shape[2]
+    bm, bm_stride = _map_of(blockmap, q, n_k, block)
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    with torch.cuda.device(q.device), _on(stream):
+        o = torch.empty_like(q) if out is None else out
+        _check_q(o, "out", q)
+        lse = torch.empty((b, h, n_q), dtype=torch.float32, device=q.device) if return_lse else None
+        L = _lib.lib()
+        ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_workspace_size(b, h, d, n_q, n_k, int(block))), q.device)
+        _lib.check(L.psa_attention_map_fwd(_ptr(q), kv, _ptr(o), b, h, d, n_q, n_k, int(block), bm, bm_stride, scale,
+                                           _ptr(lse), ws, nbytes, _stream(None, q.device)))
+    return (o, lse) if return_lse else o
+
+
+def attention_map_bwd(do, q, k, v, o, lse, blockmap, block, scale=None, dq=None, dk=None, dv=None, workspace=None,
+                      stream=None):
+    """Gradients of attention_map_fwd (psa_attention_map_bwd) from do, the gradient of o, and the forward's o and
+    lse; the other arguments are the forward's.  Returns (dq, dk, dv), contiguous; those of a shared key head are
+    the sums over its query heads."""
+    torch = _torch()
+    _check_q(q)
+    _check_q(do, "do", q)
+    _check_q(o, "o", q)
+    kv = _kv(q, k, v)
+    b, h, n_q, d = q.shape
+    n_k = k.shape[2]
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (b, h, n_q) or not lse.is_contiguous() or lse.device != q.device:
+        raise ValueError("lse must be a contiguous float32 tensor [batch, heads, N_q] on the queries' device")
+    bm, bm_stride = _map_of(blockmap, q, n_k, block)
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    with torch.cuda.device(q.device), _on(stream):
+        dq = torch.empty_like(q) if dq is None else dq
+        dk = torch.empty(k.shape, dtype=k.dtype, device=q.device) if dk is None else dk
+        dv = torch.empty(k.shape, dtype=k.dtype, device=q.device) if dv is None else dv
+        _check_q(dq, "dq", q)
+        _check_q(dk, "dk", k)
+        _check_q(dv, "dv", k)
+        L = _lib.lib()
+        ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_bwd_workspace_size(b, h, d, n_q, int(block))), q.device)
+        _lib.check(L.psa_attention_map_bwd(_ptr(do), _ptr(q), kv, _ptr(o), _ptr(lse), b, h, d, n_q, n_k, int(block), bm,
+                                           bm_stride, scale, _ptr(dq), _ptr(dk), _ptr(dv), ws, nbytes,
+                                           _stream(None, q.device)))
+    return dq, dk, dv

@@ -34,6 +34,8 @@ EXPORTS = ("psa_num_blocks", "psa_workspace_size", "psa_build_blockmap", "psa_at
            "psa_to_blocks", "psa_from_blocks", "psa_build_blockmap_3d", "psa_workspace_size_3d",
            "psa_attention_plan_3d", "psa_attention_run_3d", "psa_l2_workspace_size", "psa_l2_distance",
            "psa_qk_norm_rope_fwd", "psa_qk_norm_rope_workspace_size", "psa_qk_norm_rope_bwd",
+           "psa_select_workspace_size", "psa_select_blocks", "psa_attention_map_workspace_size",
+           "psa_attention_map_fwd", "psa_attention_map_bwd_workspace_size", "psa_attention_map_bwd",
            "psa_status_string", "psa_last_error")
 
 
@@ -60,6 +62,11 @@ class Rope(ctypes.Structure):
     _fields_ = [("grid", Grid), ("origin_t", ctypes.c_int32), ("origin_h", ctypes.c_int32),
                 ("origin_w", ctypes.c_int32), ("axis_t", ctypes.c_int32), ("axis_h", ctypes.c_int32),
                 ("axis_w", ctypes.c_int32), ("pairs", ctypes.c_int32), ("theta", ctypes.c_double)]
+
+
+class Kv(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
 
 
 class PsaError(RuntimeError):
@@ -140,6 +147,20 @@ def lib():
         L.psa_qk_norm_rope_bwd.argtypes = [vp, vp, rows, rows, rows, rows, vp, vp, i32, i32, i32, rope, i32, vp, vp,
                                            ctypes.c_float, vp, sz, vp]
         L.psa_qk_norm_rope_bwd.restype = ctypes.c_int
+        kv = ctypes.POINTER(Kv)
+        L.psa_select_workspace_size.argtypes = [i32] * 7
+        L.psa_select_workspace_size.restype = sz
+        L.psa_select_blocks.argtypes = [vp, kv] + [i32] * 9 + [vp, vp, vp, sz, vp]
+        L.psa_select_blocks.restype = ctypes.c_int
+        L.psa_attention_map_workspace_size.argtypes = [i32] * 6
+        L.psa_attention_map_workspace_size.restype = sz
+        L.psa_attention_map_fwd.argtypes = [vp, kv, vp] + [i32] * 6 + [vp, i64, ctypes.c_float, vp, vp, sz, vp]
+        L.psa_attention_map_fwd.restype = ctypes.c_int
+        L.psa_attention_map_bwd_workspace_size.argtypes = [i32] * 5
+        L.psa_attention_map_bwd_workspace_size.restype = sz
+        L.psa_attention_map_bwd.argtypes = [vp, vp, kv, vp, vp] + [i32] * 6 + [vp, i64, ctypes.c_float, vp, vp, vp,
+                                                                              vp, sz, vp]
+        L.psa_attention_map_bwd.restype = ctypes.c_int
         L.psa_status_string.argtypes = [ctypes.c_int]
         L.psa_status_string.restype = ctypes.c_char_p
         L.psa_last_error.argtypes = []

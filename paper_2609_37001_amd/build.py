@@ -12,7 +12,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libpsa.so")
-SOURCES = ("psa_api.hip", "psa_kernels.hip", "psa_rope.hip")
+SOURCES = ("psa_api.hip", "psa_kernels.hip", "psa_rope.hip", "psa_select.hip", "psa_map.hip")
 ARCH = "gfx950"
 
 

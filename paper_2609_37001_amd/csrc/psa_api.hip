@@ -337,6 +337,78 @@ void set_rows(psa::RopeTensor* t, const psa_rows_t& r) {
   t->n_heads = r.n_heads;
 }
 
+// Shapes that a selection and the attention over a map share.  kv may be null (size queries).
+psa_status_t check_mapped(int32_t batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_q,
+                          int32_t n_k, int32_t block, int32_t* nbq, int32_t* nbk) {
+  psa_status_t s = check_attention_shape(batch, n_heads, head_dim, block);
+  if (s != PSA_OK) return s;
+  if (n_kv_heads < 1 || n_heads % n_kv_heads)
+    return fail(PSA_ERR_INVALID, "%d key heads do not divide %d query heads", n_kv_heads, n_heads);
+  if (n_q < 1 || n_k < 1) return fail(PSA_ERR_INVALID, "n_q and n_k must be >= 1 (got %d, %d)", n_q, n_k);
+  *nbq = (int32_t)(((int64_t)n_q + block - 1) / block);
+  *nbk = (int32_t)(((int64_t)n_k + block - 1) / block);
+  if (*nbq > PSA_MAX_BLOCKS || *nbk > PSA_MAX_BLOCKS)
+    return fail(PSA_ERR_UNSUPPORTED, "%d x %d blocks exceed %d", *nbq, *nbk, PSA_MAX_BLOCKS);
+  // (work items, and blocks of both sides together, are 32-bit numbers)
+  if ((int64_t)batch * n_heads * ((int64_t)*nbq + *nbk) >= ((int64_t)1 << 31) - 8)
+    return fail(PSA_ERR_UNSUPPORTED, "too many work items");
+  return PSA_OK;
+}
+
+psa_status_t check_kv(const psa_kv_t* kv, bool values) {
+  if (!kv || !kv->k || (values && !kv->v)) return fail(PSA_ERR_INVALID, "keys and values must be non-NULL");
+  if (!aligned(kv->k, 16) || (values && !aligned(kv->v, 16)))
+    return fail(PSA_ERR_INVALID, "keys and values must be 16-byte aligned (%p %p)", kv->k, kv->v);
+  if (kv->stride_b < 0 || kv->stride_h < 0 || kv->stride_b % 8 || kv->stride_h % 8)
+    return fail(PSA_ERR_INVALID, "strides of keys and values must be multiples of 8, not negative (%lld, %lld)",
+                (long long)kv->stride_b, (long long)kv->stride_h);
+  return PSA_OK;
+}
+
+// Tensors, map and shapes of an attention over a map; fills `a` but for what one direction has alone.
+psa_status_t check_map_call(const void* q, const psa_kv_t* kv, const void* o, const float* lse, int32_t batch,
+                            int32_t n_heads, int32_t head_dim, int32_t n_q, int32_t n_k, int32_t block,
+                            const uint8_t* blockmap, int64_t map_stride_b, float softmax_scale, psa::MapArgs* a) {
+  psa_status_t s = check_kv(kv, true);
+  if (s != PSA_OK) return s;
+  int32_t nbq, nbk;
+  s = check_mapped(batch, n_heads, kv->n_heads, head_dim, n_q, n_k, block, &nbq, &nbk);
+  if (s != PSA_OK) return s;
+  if (!q || !o || !aligned(q, 16) || !aligned(o, 16))
+    return fail(PSA_ERR_INVALID, "q and o must be non-NULL and 16-byte aligned (%p %p)", q, o);
+  if (!aligned(lse, 4)) return fail(PSA_ERR_INVALID, "lse must be 4-byte aligned (%p)", (const void*)lse);
+  if (!blockmap) return fail(PSA_ERR_INVALID, "blockmap is NULL");
+  if (map_stride_b < 0) return fail(PSA_ERR_INVALID, "map_stride_b must not be negative (%lld)", (long long)map_stride_b);
+  *a = psa::MapArgs{};
+  a->q = (const __bf16*)q;
+  a->k = (const __bf16*)kv->k;
+  a->v = (const __bf16*)kv->v;
+  a->o = (__bf16*)const_cast<void*>(o);
+  a->lse = const_cast<float*>(lse);
+  a->map = blockmap;
+  a->map_stride_b = map_stride_b;
+  a->kv_stride_b = kv->stride_b;
+  a->kv_stride_h = kv->stride_h;
+  a->n_bh = batch * n_heads;
+  a->n_heads = n_heads;
+  a->group = n_heads / kv->n_heads;
+  a->n_q = n_q;
+  a->n_k = n_k;
+  a->nbq = nbq;
+  a->nbk = nbk;
+  a->block = block;
+  a->scale = softmax_scale;
+  a->c = softmax_scale * 1.4426950408889634f;
+  return PSA_OK;
+}
+
+psa_status_t check_map_workspace(const void* workspace, size_t bytes, size_t need) {
+  if (need && (!workspace || bytes < need))
+    return fail(PSA_ERR_WORKSPACE, "workspace of %zu bytes at %p; %zu bytes required", bytes, workspace, need);
+  if (!aligned(workspace, 256)) return fail(PSA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  return PSA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -672,6 +744,119 @@ psa_status_t psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const 
   const hipError_t e = psa::launch_norm_rope_bwd(a, head_dim, type == PSA_TYPE_FP32, norm,
                                                  rope->pairs == PSA_PAIRS_HALVES, dq_weight, dk_weight, stream);
   return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_qk_norm_rope_bwd launch");
+}
+
+size_t psa_select_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t n_q, int32_t n_k, int32_t block) {
+  const SavedError keep;
+  int32_t nbq, nbk;
+  if (check_mapped(batch, n_heads, n_kv_heads, head_dim, n_q, n_k, block, &nbq, &nbk) != PSA_OK) return 0;
+  return psa::select_layout(batch * n_heads, batch * n_kv_heads, head_dim, nbq, nbk).total;
+}
+
+psa_status_t psa_select_blocks(const void* q, const psa_kv_t* kv, int32_t batch, int32_t n_heads,
+                               int32_t head_dim, int32_t n_q, int32_t n_k, int32_t block, int32_t keep,
+                               int32_t q_text, int32_t k_text, uint8_t* blockmap, int32_t* kept_per_row,
+                               void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  psa_status_t s = check_kv(kv, false);
+  if (s != PSA_OK) return s;
+  psa::SelectArgs a = {};
+  s = check_mapped(batch, n_heads, kv->n_heads, head_dim, n_q, n_k, block, &a.nbq, &a.nbk);
+  if (s != PSA_OK) return s;
+  if (!q || !aligned(q, 16)) return fail(PSA_ERR_INVALID, "q must be non-NULL and 16-byte aligned (%p)", q);
+  if (!blockmap) return fail(PSA_ERR_INVALID, "blockmap is NULL");
+  s = check_counts_out(kept_per_row, nullptr);
+  if (s != PSA_OK) return s;
+  if (keep < 0) return fail(PSA_ERR_INVALID, "keep must be >= 0 (got %d)", keep);
+  if (q_text < 0 || q_text > n_q || k_text < 0 || k_text > n_k)
+    return fail(PSA_ERR_INVALID, "text of %d and %d tokens in %d and %d", q_text, k_text, n_q, n_k);
+  const psa::SelectLayout l = psa::select_layout(batch * n_heads, batch * kv->n_heads, head_dim, a.nbq, a.nbk);
+  s = check_map_workspace(workspace, workspace_bytes, l.total);
+  if (s != PSA_OK) return s;
+  a.q = (const __bf16*)q;
+  a.k = (const __bf16*)kv->k;
+  a.kv_stride_b = kv->stride_b;
+  a.kv_stride_h = kv->stride_h;
+  a.mean_q = (double*)((char*)workspace + l.mean_q);
+  a.mean_k = (double*)((char*)workspace + l.mean_k);
+  a.scores = (uint64_t*)((char*)workspace + l.scores);
+  a.map = blockmap;
+  a.kept_per_row = kept_per_row;
+  a.n_bh = batch * n_heads;
+  a.n_heads = n_heads;
+  a.n_kv_heads = kv->n_heads;
+  a.group = n_heads / kv->n_heads;
+  a.n_q = n_q;
+  a.n_k = n_k;
+  a.block = block;
+  a.keep = keep;
+  a.first_q = q_text ? (n_q - q_text) / block : a.nbq;
+  a.first_k = k_text ? (n_k - k_text) / block : a.nbk;
+  const hipError_t e = psa::launch_select(a, head_dim, stream);
+  return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_select_blocks launch");
+}
+
+size_t psa_attention_map_workspace_size(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_q,
+                                        int32_t n_k, int32_t block) {
+  const SavedError keep;
+  int32_t nbq, nbk;
+  if (check_mapped(batch, n_heads, 1, head_dim, n_q, n_k, block, &nbq, &nbk) != PSA_OK) return 0;
+  return psa::map_layout(batch * n_heads, head_dim, nbq, nbk, block).total;
+}
+
+psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, int32_t batch,
+                                   int32_t n_heads, int32_t head_dim, int32_t n_q, int32_t n_k,
+                                   int32_t block, const uint8_t* blockmap, int64_t map_stride_b,
+                                   float softmax_scale, float* lse, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream) {
+  psa::MapArgs a;
+  psa_status_t s = check_map_call(q, kv, o, lse, batch, n_heads, head_dim, n_q, n_k, block, blockmap, map_stride_b,
+                                  softmax_scale, &a);
+  if (s != PSA_OK) return s;
+  const psa::MapLayout l = psa::map_layout(a.n_bh, head_dim, a.nbq, a.nbk, block);
+  s = check_map_workspace(workspace, workspace_bytes, l.total);
+  if (s != PSA_OK) return s;
+  a.parts = l.parts;
+  a.part_o = (float*)workspace;
+  a.part_ml = (float2*)((char*)workspace + l.part_ml);
+  const hipError_t e = psa::launch_map_fwd(a, head_dim, stream);
+  return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_attention_map_fwd launch");
+}
+
+size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_q,
+                                            int32_t block) {
+  const SavedError keep;
+  int32_t nbq, nbk;
+  if (check_mapped(batch, n_heads, 1, head_dim, n_q, 1, block, &nbq, &nbk) != PSA_OK) return 0;
+  return psa::map_bwd_layout(batch * n_heads, head_dim, n_q, nbq, block).total;
+}
+
+psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_kv_t* kv, const void* o,
+                                   const float* lse, int32_t batch, int32_t n_heads, int32_t head_dim,
+                                   int32_t n_q, int32_t n_k, int32_t block, const uint8_t* blockmap,
+                                   int64_t map_stride_b, float softmax_scale, void* dq, void* dk,
+                                   void* dv, void* workspace, size_t workspace_bytes,
+                                   hipStream_t stream) {
+  psa::MapArgs a;
+  psa_status_t s = check_map_call(q, kv, o, lse, batch, n_heads, head_dim, n_q, n_k, block, blockmap, map_stride_b,
+                                  softmax_scale, &a);
+  if (s != PSA_OK) return s;
+  if (!lse) return fail(PSA_ERR_INVALID, "lse is NULL");
+  for (const void* p : {grad_o, (const void*)dq, (const void*)dk, (const void*)dv})
+    if (!p || !aligned(p, 16))
+      return fail(PSA_ERR_INVALID, "grad_o, dq, dk and dv must be non-NULL and 16-byte aligned (%p)", p);
+  const psa::MapBwdLayout l = psa::map_bwd_layout(a.n_bh, head_dim, n_q, a.nbq, block);
+  s = check_map_workspace(workspace, workspace_bytes, l.total);
+  if (s != PSA_OK) return s;
+  a.grad_o = (const __bf16*)grad_o;
+  a.dq = (__bf16*)dq;
+  a.dk = (__bf16*)dk;
+  a.dv = (__bf16*)dv;
+  a.q_scaled = (__bf16*)workspace;
+  a.neg_lse2 = (float*)((char*)workspace + l.neg_lse2);
+  a.neg_delta = (float*)((char*)workspace + l.neg_delta);
+  const hipError_t e = psa::launch_map_bwd(a, head_dim, stream);
+  return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_attention_map_bwd launch");
 }
 
 const char* psa_status_string(psa_status_t status) {

@@ -1,0 +1,612 @@
+// Attention over the kept blocks of any block map, forward and backward: HIP kernels for gfx950.
+//
+//   forward   S = scale q k^T over kept blocks, o = softmax(S) v, lse = log sum exp S
+//   backward  P = exp(S - lse), dP = do v^T, delta = rowsum(do * o), dS = P (dP - delta)
+//             dq = scale dS k,   dk = scale dS^T q,   dv = P^T do
+//
+// Both directions form S from the same operand, q' = bf16(scale log2(e) q), in the exp2 domain: whatever its
+// rounding does to the scores, the backward's weights are those of the forward's lse, and sum to 1.
+//
+// One workgroup takes one block of one side -- queries in the forward and for dq, keys for dk and dv -- holds its
+// rows in registers, and streams the blocks that the map keeps of the other side through LDS, double-buffered,
+// with the tile engine of psa_tile.h.  Its two groups of waves hold the same rows and take half of every streamed
+// block each; their sums are added through LDS at the end.  So a block's work is spread over twice the waves, and
+// no two blocks have to agree on what they keep.
+//   * psa_mapped_fwd_kernel   S^T = K Q^T, O^T += V^T P^T
+//   * psa_mapped_dq_kernel    S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T
+//   * psa_mapped_dkv_kernel   the same with the sides exchanged: S = Q K^T, dP = dO V^T, dV^T += dO^T P,
+//                             dK^T += Q^T dS; key heads shared by several query heads stream all of them
+// Every sum has one order, fixed by the call's sizes and its map; there are no atomics on results.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "psa_launch.h"
+#include "psa_tile.h"
+
+namespace psa {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// The kept entries of a row or column of the map (`len` bytes, `stride` apart), ascending, by all waves of the
+// workgroup.  Ends with a barrier.
+template <int W>
+__device__ __forceinline__ int32_t kept_list(const uint8_t* __restrict__ row, int64_t stride, int32_t len,
+                                             uint16_t* list, int32_t* found) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  int32_t nu = 0;
+  for (int32_t base = 0; base < len; base += W * 64) {
+    const int32_t i = base + tid;
+    const bool keep = i < len && row[i * stride] != 0;
+    const uint64_t mask = __builtin_amdgcn_ballot_w64(keep);
+    if (lane == 0) found[wave] = __builtin_popcountll(mask);
+    __syncthreads();
+    int32_t pos = nu;
+#pragma unroll
+    for (int w = 0; w < W; w++) {
+      pos += w < wave ? found[w] : 0;
+      nu += found[w];
+    }
+    if (keep) list[pos + __builtin_popcountll(mask & ((1ull << lane) - 1))] = (uint16_t)i;
+    __syncthreads();
+  }
+  return __builtin_amdgcn_readfirstlane(nu);
+}
+
+// Workgroup -> item: consecutive workgroups go to the XCDs in turn, so each XCD takes a contiguous range of the
+// items, whose blocks stream much the same other side through its L2.
+__device__ __forceinline__ int32_t item_of(int32_t blk, int32_t items) {
+  const int32_t share = (items + kNumQueues - 1) / kNumQueues;
+  const int32_t at = blk / kNumQueues, i = blk % kNumQueues * share + at;
+  return at < share && i < items ? i : -1;
+}
+
+// One 32 x 32 tile X Y^T: rows k0 .. k0 + 31 of the tile X in LDS (in the order of key_perm), this lane's row of Y
+// in registers; acc is where the sums start.
+template <int D>
+__device__ __forceinline__ f32x16 rows_times(const bf16x8 (&y)[D / 16], const uint8_t* x, int k0, int lane, f32x16 acc) {
+  constexpr int CPR = D / 8, RB = 2 * D, DC = D / 16;
+  const int h = lane >> 5, row = k0 + key_perm(lane & 31), sw = swz<CPR>(row);
+  const uint8_t* base = x + row * RB;
+#pragma unroll
+  for (int cc = 0; cc < DC; cc++)
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(base + (((2 * cc + h) ^ sw) << 4)), y[cc], acc, 0, 0, 0);
+  return acc;
+}
+
+// out^T += X^T p for the 16 rows k0 .. k0 + 15 of the tile X in LDS; p holds this lane's eight of them.
+template <int D>
+__device__ __forceinline__ void cols_times(f32x16 (&out)[D / 32], const uint8_t* x, int k0, bf16x8 p, int lane) {
+  constexpr int CPR = D / 8, RB = 2 * D, DT = D / 32;
+  const int h = lane >> 5, g = lane >> 4, j16 = lane & 15;
+  const int row = k0 + 8 * h + (j16 >> 2);
+  const int sw0 = swz<CPR>(row), sw1 = swz<CPR>(row + 4);
+#pragma unroll
+  for (int dt = 0; dt < DT; dt++) {
+    const int dd = dt * 32 + 16 * (g & 1) + 4 * (j16 & 3);
+    const int chunk = dd >> 3, inoff = (dd & 7) * 2;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PSA_LDS s16x4*)(x + row * RB + ((chunk ^ sw0) << 4) + inoff));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PSA_LDS s16x4*)(x + (row + 4) * RB + ((chunk ^ sw1) << 4) + inoff));
+    const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    out[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p, out[dt], 0, 0, 0);
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void load_rows(bf16x8 (&y)[D / 16], const __bf16* row, int h) {
+#pragma unroll
+  for (int cc = 0; cc < D / 16; cc++) y[cc] = *((const bf16x8*)row + h + 2 * cc);
+}
+
+// Where a tile's sums start: element e belongs to row 16 (e / 8) + e % 8 from `row` on.
+__device__ __forceinline__ f32x16 start_of(const float* row) {
+  f32x16 v;
+#pragma unroll
+  for (int e = 0; e < 16; e++) v[e] = row[16 * (e >> 3) + (e & 7)];
+  return v;
+}
+
+__device__ __forceinline__ bf16x8 half_of(const f32x16& v, int j) {
+  f32x8 e;
+#pragma unroll
+  for (int x = 0; x < 8; x++) e[x] = v[8 * j + x];
+  return __builtin_convertvector(e, bf16x8);
+}
+
+// Stores 32 columns of a row: O^T accumulator `v` of column group dt.
+__device__ __forceinline__ void store_cols(__bf16* dst, const f32x16& v, float f) {
+#pragma unroll
+  for (int a = 0; a < 4; a++) {
+    const f32x4 x = {v[4 * a] * f, v[4 * a + 1] * f, v[4 * a + 2] * f, v[4 * a + 3] * f};
+    *(bf16x4*)(dst + 8 * a) = __builtin_convertvector(x, bf16x4);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Forward.
+// ---------------------------------------------------------------------------------------------
+
+// SPLIT: few query blocks; `parts` workgroups share one, each takes a part of its list and leaves its sums
+// (relative to its base m, with m and l) in the workspace, where psa_mapped_join_kernel adds them.
+template <int D, int BLK, bool SPLIT>
+__global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_fwd_kernel(MapArgs a) {
+  using T = Tile<D, BLK>;
+  constexpr int HK = BLK / 2, W = 2 * T::kWaves, DH = T::DT / 2;
+  using H = Half<D, BLK, HK>;
+  __shared__ __attribute__((aligned(1024))) uint8_t sk[2][T::BYTES];
+  __shared__ __attribute__((aligned(1024))) uint8_t sv[2][T::BYTES];
+  __shared__ int32_t found[W];
+  __shared__ float2 stat[W][32];              // (m, l) of every wave's rows
+  extern __shared__ uint16_t list[];          // nbk entries
+
+  const int32_t items = a.n_bh * a.nbq * (SPLIT ? a.parts : 1);
+  const int32_t whole = item_of(blockIdx.x, items);
+  if (whole < 0) return;
+  const int32_t item = SPLIT ? whole / a.parts : whole, part = SPLIT ? whole - item * a.parts : 0;
+  const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
+  const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
+  const int h = lane >> 5, r32 = lane & 31;
+  const int64_t kv_off = b * a.kv_stride_b + (hd / a.group) * a.kv_stride_h;
+  const __bf16 *kh = a.k + kv_off, *vh = a.v + kv_off;
+  const int32_t n = a.n_k, n_q = a.n_q;
+  const int row = qb * BLK + gw * 32 + r32;
+  // whether any of this wave's rows exists
+  const bool rows = __builtin_amdgcn_readfirstlane(qb * BLK + gw * 32) < n_q;
+
+  int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk, 1, a.nbk, list, found);
+  int32_t first = 0;
+  if constexpr (SPLIT) {
+    first = (int32_t)((int64_t)nu * part / a.parts);
+    nu = (int32_t)((int64_t)nu * (part + 1) / a.parts) - first;
+  }
+  auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[first + i]); };
+
+  DmaPlan<D, BLK> plan;
+  plan.init(__builtin_amdgcn_readfirstlane(wave), lane);
+  int kb = 0;
+  if (nu > 0) {
+    kb = entry(0);
+    issue_block<D, BLK>(plan, kh, lds_address(sk[0]), kb, n);
+    issue_block<D, BLK>(plan, vh, lds_address(sv[0]), kb, n);
+  }
+  WaveState<D, BLK> st;
+  {
+    load_rows<D>(st.q, a.q + ((int64_t)bh * n_q + min(row, n_q - 1)) * D, h);
+#pragma unroll
+    for (int cc = 0; cc < T::DC; cc++)
+      st.q[cc] = __builtin_convertvector(__builtin_convertvector(st.q[cc], f32x8) * a.c, bf16x8);
+#pragma unroll
+    for (int cc = 0; cc < T::DC; cc++) asm volatile("" ::"v"(st.q[cc]));
+  }
+  st.m = -__builtin_inff();
+  st.l = 0.0f;
+  st.set_neg_max(0.0f);
+  int fresh = 1;
+#pragma unroll
+  for (int dt = 0; dt < T::DT; dt++) st.o[dt] = (f32x16){};
+
+  const int k0 = grp * HK;
+  for (int i = 0; i < nu; i++) {
+    const bool tail = (kb + 1) * BLK > n;
+    wait_dma<0>();                                        // block i, issued a block ago
+    __syncthreads();                                      // ... by every wave; block i-1 read
+    const int cur = kb;
+    const bool more = i + 1 < nu;
+    if (more) {
+      kb = entry(i + 1);
+      issue_block<D, BLK>(plan, kh, lds_address(sk[(i + 1) & 1]), kb, n);
+    }
+    if (rows) {
+      f32x16 s[H::KT];
+      qk_half<D, BLK, HK>(st, s, sk[i & 1], k0, lane);
+      if (more) issue_block<D, BLK>(plan, vh, lds_address(sv[(i + 1) & 1]), kb, n);
+      softmax_pv_half<D, BLK, false, HK>(st, s, sv[i & 1], cur, k0, n, tail, ~0ull, ~0ull, lane, fresh);
+    } else if (more) {
+      issue_block<D, BLK>(plan, vh, lds_address(sv[(i + 1) & 1]), kb, n);
+    }
+  }
+
+  // Merge: both groups scale their O to the common base; group g finishes columns 32 DH g .., adding what the
+  // other group holds of them.
+  const float mine = pair_sum(st.l);
+  if (h == 0) stat[wave][r32] = make_float2(st.m, mine);
+  __syncthreads();                                        // (also: the buffers are no longer read)
+  const float2 other = stat[(1 - grp) * T::kWaves + gw][r32];
+  const float top = fmaxf(st.m, other.x);
+  const float alpha = st.m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(st.m - top);
+  const float beta = other.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(other.x - top);
+  const float lsum = mine * alpha + other.y * beta;
+  const float inv = SPLIT ? 1.0f : lsum > 0.0f ? 1.0f / lsum : 0.0f;
+  static_assert(W * DH * 4096 <= 4 * T::BYTES, "a wave's half of O fits its share of the buffers");
+  constexpr int kPer = T::BYTES / (DH * 4096);            // waves per buffer
+  auto slot = [&](int w) { return (f32x4*)((w / kPer < 2 ? sk[w / kPer] : sv[w / kPer - 2]) + (w % kPer) * DH * 4096) + lane; };
+  f32x4* out = slot(wave);
+#pragma unroll
+  for (int j = 0; j < DH; j++)
+#pragma unroll
+    for (int x = 0; x < 4; x++) {
+      const f32x16 &lo = st.o[j], &hi = st.o[DH + j];
+      const int e = 4 * x;
+      const f32x4 lower = {lo[e], lo[e + 1], lo[e + 2], lo[e + 3]}, upper = {hi[e], hi[e + 1], hi[e + 2], hi[e + 3]};
+      out[(j * 4 + x) * 64] = (grp == 0 ? upper : lower) * alpha;
+    }
+  __syncthreads();
+  const f32x4* in = slot((1 - grp) * T::kWaves + gw);
+  const int64_t place = SPLIT ? (int64_t)whole * BLK + gw * 32 + r32 : (int64_t)bh * n_q + row;
+  const int64_t at = place * D + 32 * DH * grp + 4 * h;
+#pragma unroll
+  for (int j = 0; j < DH; j++)
+#pragma unroll
+    for (int x = 0; x < 4; x++) {
+      const f32x16 &lo = st.o[j], &hi = st.o[DH + j];
+      const int e = 4 * x;
+      const f32x4 lower = {lo[e], lo[e + 1], lo[e + 2], lo[e + 3]}, upper = {hi[e], hi[e + 1], hi[e + 2], hi[e + 3]};
+      const f32x4 sum = ((grp == 0 ? lower : upper) * alpha + in[(j * 4 + x) * 64]) * inv;
+      if (row < n_q) {
+        if constexpr (SPLIT)
+          *(f32x4*)(a.part_o + at + 32 * j + 8 * x) = sum;
+        else
+          *(bf16x4*)(a.o + at + 32 * j + 8 * x) = __builtin_convertvector(sum, bf16x4);
+      }
+    }
+  if (grp == 0 && h == 0 && row < n_q) {
+    if constexpr (SPLIT)
+      a.part_ml[place] = make_float2(top, lsum);
+    else if (a.lse)
+      a.lse[place] = lsum > 0.0f ? (top + __builtin_log2f(lsum)) * 0.69314718055994530942f : -__builtin_inff();
+  }
+}
+
+// Adds the parts of every query row: o = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p.  D / 4 lanes a row.
+template <int D, int BLK>
+__global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
+  constexpr int L = D / 4;
+  const int64_t r = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  if (r >= (int64_t)a.n_bh * a.n_q) return;
+  const int c = threadIdx.x % L;
+  const int32_t bh = (int32_t)(r / a.n_q), row = (int32_t)(r - (int64_t)bh * a.n_q), qb = row / BLK;
+  const int64_t first = ((int64_t)bh * a.nbq + qb) * a.parts * BLK + (row - qb * BLK);
+  float m = -__builtin_inff();
+  for (int p = 0; p < a.parts; p++) m = fmaxf(m, a.part_ml[first + (int64_t)p * BLK].x);
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  float l = 0.0f;
+#pragma unroll 4
+  for (int p = 0; p < a.parts; p++) {
+    const int64_t at = first + (int64_t)p * BLK;
+    const float2 ml = a.part_ml[at];
+    const float w = ml.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
+    l += w * ml.y;
+    o += *(const f32x4*)(a.part_o + at * D + 4 * c) * w;
+  }
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  *(bf16x4*)(a.o + r * D + 4 * c) = __builtin_convertvector(o * inv, bf16x4);
+  if (a.lse && c == 0) a.lse[r] = l > 0.0f ? (m + __builtin_log2f(l)) * 0.69314718055994530942f : -__builtin_inff();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Backward.
+// ---------------------------------------------------------------------------------------------
+
+// Per query row, in blocks of `block` rows: -lse log2(e) and -delta, where the sums of S and dP start; and q'.  Rows
+// behind the last one, and rows that keep nothing (lse = -inf), get -inf: every weight formed with it is 0.
+// D / 8 lanes a row.
+template <int D>
+__global__ __launch_bounds__(256) void psa_mapped_rows_kernel(MapArgs a) {
+  constexpr int L = D / 8;
+  const int64_t r = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  const int32_t padded = a.nbq * a.block;
+  if (r >= (int64_t)a.n_bh * padded) return;
+  const int c = threadIdx.x % L;
+  const int32_t bh = (int32_t)(r / padded), row = (int32_t)(r - (int64_t)bh * padded);
+  const int64_t at = (int64_t)bh * a.n_q + min(row, a.n_q - 1);
+  const f32x8 x = __builtin_convertvector(*(const bf16x8*)(a.grad_o + at * D + 8 * c), f32x8);
+  const f32x8 y = __builtin_convertvector(*(const bf16x8*)(a.o + at * D + 8 * c), f32x8);
+  const f32x8 q = __builtin_convertvector(*(const bf16x8*)(a.q + at * D + 8 * c), f32x8);
+  float s = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; e++) s = fmaf(x[e], y[e], s);
+#pragma unroll
+  for (int off = L / 2; off > 0; off >>= 1) s += __shfl_xor(s, off);
+  if (row < a.n_q) *(bf16x8*)(a.q_scaled + at * D + 8 * c) = __builtin_convertvector(q * a.c, bf16x8);
+  if (c == 0) {
+    const float lse = a.lse[at];
+    const bool none = row >= a.n_q || lse == -__builtin_inff();
+    a.neg_lse2[r] = none ? -__builtin_inff() : -lse * kLog2e;
+    a.neg_delta[r] = none ? 0.0f : -s;
+  }
+}
+
+template <int D, int BLK>
+__global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_dq_kernel(MapArgs a) {
+  using T = Tile<D, BLK>;
+  constexpr int HK = BLK / 2, W = 2 * T::kWaves, DH = T::DT / 2;
+  __shared__ __attribute__((aligned(1024))) uint8_t sk[2][T::BYTES];
+  __shared__ __attribute__((aligned(1024))) uint8_t sv[2][T::BYTES];
+  __shared__ int32_t found[W];
+  extern __shared__ uint16_t list[];          // nbk entries
+
+  const int32_t item = item_of(blockIdx.x, a.n_bh * a.nbq);
+  if (item < 0) return;
+  const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
+  const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
+  const int h = lane >> 5, r32 = lane & 31;
+  const int64_t kv_off = b * a.kv_stride_b + (hd / a.group) * a.kv_stride_h;
+  const __bf16 *kh = a.k + kv_off, *vh = a.v + kv_off;
+  const int32_t n = a.n_k, n_q = a.n_q;
+  const int row = qb * BLK + gw * 32 + r32;
+
+  const int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk, 1, a.nbk, list, found);
+  auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[i]); };
+  DmaPlan<D, BLK> plan;
+  plan.init(__builtin_amdgcn_readfirstlane(wave), lane);
+  int kb = 0;
+  if (nu > 0) {
+    kb = entry(0);
+    issue_block<D, BLK>(plan, kh, lds_address(sk[0]), kb, n);
+    issue_block<D, BLK>(plan, vh, lds_address(sv[0]), kb, n);
+  }
+  bf16x8 q[T::DC], g[T::DC];
+  const int64_t at = ((int64_t)bh * n_q + min(row, n_q - 1)) * D;
+  load_rows<D>(q, a.q_scaled + at, h);
+  load_rows<D>(g, a.grad_o + at, h);
+  const int64_t sat = (int64_t)bh * a.nbq * BLK + row;
+  const float neg_lse2 = a.neg_lse2[sat], neg_delta = a.neg_delta[sat];
+  f32x16 dq[T::DT];
+#pragma unroll
+  for (int dt = 0; dt < T::DT; dt++) dq[dt] = (f32x16){};
+
+  for (int i = 0; i < nu; i++) {
+    const bool tail = (kb + 1) * BLK > n;
+    wait_dma<0>();
+    __syncthreads();
+    const int cur = kb;
+    const bool more = i + 1 < nu;
+    if (more) {
+      kb = entry(i + 1);
+      issue_block<D, BLK>(plan, kh, lds_address(sk[(i + 1) & 1]), kb, n);
+      issue_block<D, BLK>(plan, vh, lds_address(sv[(i + 1) & 1]), kb, n);
+    }
+#pragma unroll
+    for (int kt = 0; kt < HK / 32; kt++) {
+      const int k0 = grp * HK + 32 * kt;
+      f32x16 s = rows_times<D>(q, sk[i & 1], k0, lane, (f32x16){} + neg_lse2);
+      f32x16 dp = rows_times<D>(g, sv[i & 1], k0, lane, (f32x16){} + neg_delta);
+      if (tail) {
+        // Keys behind the last one read as the last one, whose weight is finite: no gradient of theirs.
+        asm volatile("" ::: "memory");        // keep the mask a branch taken only by the last block
+        const int kbase = cur * BLK + k0 + 8 * h;
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+          if (kbase + 16 * (e >> 3) + (e & 7) >= n) dp[e] = 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e++) dp[e] *= __builtin_amdgcn_exp2f(s[e]);
+#pragma unroll
+      for (int j = 0; j < 2; j++) cols_times<D>(dq, sk[i & 1], k0 + 16 * j, half_of(dp, j), lane);
+    }
+  }
+
+  // Group g finishes columns 32 DH g .., adding what the other group holds of them.
+  __syncthreads();                                        // the buffers are no longer read
+  constexpr int kPer = T::BYTES / (DH * 4096);            // waves per buffer
+  auto slot = [&](int w) { return (f32x4*)((w / kPer < 2 ? sk[w / kPer] : sv[w / kPer - 2]) + (w % kPer) * DH * 4096) + lane; };
+  f32x4* out = slot(wave);
+#pragma unroll
+  for (int j = 0; j < DH; j++)
+#pragma unroll
+    for (int x = 0; x < 4; x++)
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        out[(j * 4 + x) * 64][e] = grp == 0 ? dq[DH + j][4 * x + e] : dq[j][4 * x + e];
+  __syncthreads();
+  const f32x4* in = slot((1 - grp) * T::kWaves + gw);
+  if (row < n_q) {
+    __bf16* dst = a.dq + ((int64_t)bh * n_q + row) * D + 32 * DH * grp + 4 * h;
+#pragma unroll
+    for (int j = 0; j < DH; j++) {
+      f32x16 v;
+#pragma unroll
+      for (int x = 0; x < 4; x++)
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+          v[4 * x + e] = (grp == 0 ? dq[j][4 * x + e] : dq[DH + j][4 * x + e]) + in[(j * 4 + x) * 64][e];
+      store_cols(dst + 32 * j, v, a.scale);
+    }
+  }
+}
+
+template <int D, int BLK>
+__global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_dkv_kernel(MapArgs a) {
+  using T = Tile<D, BLK>;
+  constexpr int HQ = BLK / 2, W = 2 * T::kWaves;
+  __shared__ __attribute__((aligned(1024))) uint8_t sq[2][T::BYTES];
+  __shared__ __attribute__((aligned(1024))) uint8_t sg[2][T::BYTES];
+  __shared__ __attribute__((aligned(16))) float stat[2][2][BLK];       // -lse log2(e) and -delta of a streamed block
+  __shared__ int32_t found[W];
+  extern __shared__ uint16_t list[];          // nbq entries
+
+  const int32_t item = item_of(blockIdx.x, a.n_bh / a.group * a.nbk);
+  if (item < 0) return;
+  const int32_t bk = item / a.nbk, kb = item - bk * a.nbk, n_kv = a.n_heads / a.group;
+  const int32_t b = bk / n_kv, hk = bk - b * n_kv;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
+  const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
+  const int h = lane >> 5, r32 = lane & 31;
+  const int32_t n_q = a.n_q, n_k = a.n_k;
+  const int key = kb * BLK + gw * 32 + r32;
+  bf16x8 k[T::DC], v[T::DC];
+  {
+    const int64_t at = b * a.kv_stride_b + hk * a.kv_stride_h + (int64_t)min(key, n_k - 1) * D;
+    load_rows<D>(k, a.k + at, h);
+    load_rows<D>(v, a.v + at, h);
+  }
+  f32x16 dk[T::DT], dv[T::DT];
+#pragma unroll
+  for (int dt = 0; dt < T::DT; dt++) dk[dt] = dv[dt] = (f32x16){};
+  DmaPlan<D, BLK> plan;
+  plan.init(__builtin_amdgcn_readfirstlane(wave), lane);
+
+  for (int32_t hd = hk * a.group; hd < (hk + 1) * a.group; hd++) {
+    const int64_t bh = (int64_t)b * a.n_heads + hd;
+    const __bf16 *qh = a.q_scaled + bh * n_q * D, *gh = a.grad_o + bh * n_q * D;
+    const float* sh = (tid < BLK ? a.neg_lse2 : a.neg_delta) + bh * a.nbq * BLK;
+    // (its barriers also separate the buffers from the head before)
+    const int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + (int64_t)hd * a.nbq * a.nbk + kb, a.nbk, a.nbq, list, found);
+    auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[i]); };
+    float next = 0.0f;
+    auto issue = [&](int i) {
+      const int qb = entry(i);
+      issue_block<D, BLK>(plan, qh, lds_address(sq[i & 1]), qb, n_q);
+      issue_block<D, BLK>(plan, gh, lds_address(sg[i & 1]), qb, n_q);
+      if (tid < 2 * BLK) next = sh[qb * BLK + (tid & (BLK - 1))];
+    };
+    auto put = [&](int i) {
+      if (tid < 2 * BLK) stat[i & 1][tid / BLK][tid & (BLK - 1)] = next;
+    };
+    if (nu > 0) {
+      issue(0);
+      put(0);
+    }
+    for (int i = 0; i < nu; i++) {
+      wait_dma<0>();
+      __syncthreads();
+      const bool more = i + 1 < nu;
+      if (more) issue(i + 1);
+      const uint8_t *tq = sq[i & 1], *tg = sg[i & 1];
+#pragma unroll
+      for (int kt = 0; kt < HQ / 32; kt++) {
+        const int q0 = grp * HQ + 32 * kt;
+        f32x16 s = rows_times<D>(k, tq, q0, lane, start_of(&stat[i & 1][0][q0 + 8 * h]));
+        bf16x8 p[2];
+#pragma unroll
+        for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(s[e]);
+#pragma unroll
+        for (int j = 0; j < 2; j++) p[j] = half_of(s, j);
+#pragma unroll
+        for (int j = 0; j < 2; j++) cols_times<D>(dv, tg, q0 + 16 * j, p[j], lane);
+        f32x16 dp = rows_times<D>(v, tg, q0, lane, start_of(&stat[i & 1][1][q0 + 8 * h]));
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+          const f32x8 pf = __builtin_convertvector(p[j], f32x8);
+#pragma unroll
+          for (int e = 0; e < 8; e++) dp[8 * j + e] *= pf[e];
+        }
+#pragma unroll
+        for (int j = 0; j < 2; j++) cols_times<D>(dk, tq, q0 + 16 * j, half_of(dp, j), lane);
+      }
+      if (more) put(i + 1);
+    }
+  }
+
+  // Group 0 finishes dv, group 1 dk, adding what the other group holds.
+  __syncthreads();                                        // the buffers are no longer read
+  constexpr int kPer = T::BYTES / (T::DT * 4096);         // waves per buffer
+  static_assert(kPer >= 1 && W <= 4 * kPer, "a wave's sums fit its share of the buffers");
+  auto slot = [&](int w) { return (f32x4*)((w / kPer < 2 ? sq[w / kPer] : sg[w / kPer - 2]) + (w % kPer) * T::DT * 4096) + lane; };
+  f32x4* out = slot(wave);
+#pragma unroll
+  for (int j = 0; j < T::DT; j++)
+#pragma unroll
+    for (int x = 0; x < 4; x++)
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        out[(j * 4 + x) * 64][e] = grp == 0 ? dk[j][4 * x + e] : dv[j][4 * x + e];
+  __syncthreads();
+  const f32x4* in = slot((1 - grp) * T::kWaves + gw);
+  if (key < n_k) {
+    __bf16* dst = (grp == 0 ? a.dv : a.dk) + ((int64_t)bk * n_k + key) * D + 4 * h;
+#pragma unroll
+    for (int j = 0; j < T::DT; j++) {
+      f32x16 t;
+#pragma unroll
+      for (int x = 0; x < 4; x++)
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+          t[4 * x + e] = (grp == 0 ? dv[j][4 * x + e] : dk[j][4 * x + e]) + in[(j * 4 + x) * 64][e];
+      store_cols(dst + 32 * j, t, grp == 0 ? 1.0f : 0.69314718055994530942f);   // (scale q = ln 2 q')
+    }
+  }
+}
+
+int32_t grid_of(int32_t items) { return (items + kNumQueues - 1) / kNumQueues * kNumQueues; }
+
+int32_t list_bytes(int32_t nb) { return (2 * nb + 15) & ~15; }
+
+template <typename F>
+hipError_t by_shape(int32_t head_dim, int32_t block, F f) {
+  using I64 = std::integral_constant<int, 64>;
+  using I128 = std::integral_constant<int, 128>;
+  if (head_dim == 128) return block == 128 ? f(I128(), I128()) : f(I128(), I64());
+  return block == 128 ? f(I64(), I128()) : f(I64(), I64());
+}
+
+}  // namespace
+
+// Parts of every query block's list: as many as give every CU its workgroups where there are fewer query blocks
+// (two of 64 rows to a CU, one of 128), each part at least two blocks of a full row.
+int32_t map_parts(int32_t n_bh, int32_t nbq, int32_t nbk, int32_t block) {
+  const int64_t items = (int64_t)n_bh * nbq, room = 256 * (128 / block);
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(room / items, nbk / 2));
+}
+
+MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  MapLayout l = {};
+  l.parts = map_parts(n_bh, nbq, nbk, block);
+  if (l.parts > 1) {
+    const size_t rows = (size_t)n_bh * nbq * l.parts * block;
+    l.part_ml = up(rows * head_dim * sizeof(float));
+    l.total = l.part_ml + up(rows * sizeof(float2));
+  }
+  return l;
+}
+
+MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t head_dim, int32_t n_q, int32_t nbq, int32_t block) {
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  const size_t rows = up((size_t)n_bh * nbq * block * sizeof(float));
+  MapBwdLayout l;
+  l.neg_lse2 = up((size_t)n_bh * n_q * head_dim * sizeof(__bf16));
+  l.neg_delta = l.neg_lse2 + rows;
+  l.total = l.neg_delta + rows;
+  return l;
+}
+
+hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream) {
+  return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
+    constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
+    const int32_t grid = grid_of(a.n_bh * a.nbq * a.parts);
+    if (a.parts == 1) {
+      hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, false>), dim3(grid), dim3(4 * B), list_bytes(a.nbk), stream, a);
+      return hipGetLastError();
+    }
+    hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, true>), dim3(grid), dim3(4 * B), list_bytes(a.nbk), stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t rows = (int64_t)a.n_bh * a.n_q;
+    hipLaunchKernelGGL((psa_mapped_join_kernel<D, B>), dim3((uint32_t)((rows * (D / 4) + 255) / 256)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_map_bwd(const MapArgs& a, int32_t head_dim, hipStream_t stream) {
+  return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
+    constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
+    const int64_t rows = (int64_t)a.n_bh * a.nbq * B;
+    hipLaunchKernelGGL(psa_mapped_rows_kernel<D>, dim3((uint32_t)((rows * (D / 8) + 255) / 256)), dim3(256), 0, stream, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B>), dim3(grid_of(a.n_bh / a.group * a.nbk)), dim3(4 * B),
+                       list_bytes(a.nbq), stream, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B>), dim3(grid_of(a.n_bh * a.nbq)), dim3(4 * B), list_bytes(a.nbk),
+                       stream, a);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace psa

@@ -1,0 +1,390 @@
+"""GPU parity of the attention over a block map, forward and backward, against the oracle.
+
+Forward: the parity bar of the striped attention (gpu_util).
+
+Backward tolerances.  Both sides take the same o and lse, and the oracle's scores are those of the kernel's
+operand kernel_q (with the scale ln 2, as for the forward's lse).  A weight P is off by the fp32 score and the
+exponential, 2^-17 of it; dP - delta by 2^-17 of the magnitudes it adds.  P and dS are each rounded to bf16 once or
+twice (2^-8 of the value at most each time) before they are summed, and every output once.  So an element of dq is
+off by at most 2^-8 |dq| plus the sum of (2^-8 |dS| + 2^-16 P (|do| |v| + |do| |o|)) |scale k| over the keys; dk
+likewise with twice the rounding of dS, dv with that of P; and 2^-8 of that for a rounding of the sum.  Roundings of
+unrelated values add as the root of their squares: the norm of an output's error is at most 2^-8 times the root
+of |dq|^2 plus the sum of the squared terms (a uniform rounding has 1 / sqrt(3) of its half step as its root
+mean square), beside the fp32 part.  Against the gradients of the inputs as given, pooled, the forward's bar
+holds: 1e-2 relative."""
+import numpy as np
+import pytest
+
+import oracle
+import paper_2609_37001_amd as psa
+from oracle import selection
+from workloads.inputs import bf16_round
+
+import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+INF = 0x7FFFFFFF
+
+
+def dev(x):
+    return gu.torch().from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to("cuda:0").bfloat16()
+
+
+def blocks(n, block):
+    return -(-n // block)
+
+
+def inputs(seed, b, h, hk, n_q, n_k, d):
+    rng = np.random.default_rng(seed)
+    return [bf16_round(rng.standard_normal((b, m, n, d)).astype(np.float32))
+            for m, n in ((h, n_q), (hk, n_k), (hk, n_k), (h, n_q))]
+
+
+def random_map(seed, b, h, nq, nk, density):
+    """A random map with a whole and an empty row, a whole and an empty column where there is room."""
+    rng = np.random.default_rng(seed)
+    m = (rng.random((b, h, nq, nk)) < density).astype(np.uint8)
+    if nk > 2:
+        m[:, :, :, 1] = 0
+        m[:, :, :, nk - 1] = 1
+    if nq > 2:
+        m[:, :, 1] = 1
+        m[:, :, nq - 2] = 0
+    return m
+
+
+def bits(x):
+    return x.float().cpu().numpy()
+
+
+def check_forward(q, k, v, m, block, scale, o, lse, heads, ordinary=True):
+    par = gu.Parity()
+    group = q.shape[1] // k.shape[1]
+    for bi in range(q.shape[0]):
+        for hi in heads:
+            qh, kh, vh = q[bi, hi], k[bi, hi // group], v[bi, hi // group]
+            ro, rl = selection.map_attention(qh, kh, vh, m[bi, hi], block, scale)
+            ro_k, rk = selection.map_attention(gu.kernel_q(qh, scale), kh, vh, m[bi, hi], block, gu.LN2)
+            # against the inputs as given: an element of q moves by half a step at most, 2^-8 of it
+            move = 1.01 * 2.0 ** -8 * abs(scale) * (np.abs(qh.astype(np.float64)) @ np.abs(kh.astype(np.float64)).T)
+            par.add(o[bi, hi], ro if ordinary else ro_k, lse[bi, hi], rk, rl, gu.LSE_ABS_TOL + move.max(1))
+    par.check()
+
+
+def near(got, ref, worst, fp32, squares, name):
+    """got against ref, an array of bounds, its fp32 part and the squares of the rounded terms."""
+    err = np.abs(got - ref)
+    tol = (1 + 2.0 ** -8) * (worst + 2.0 ** -8 * np.abs(ref)) + 1e-30
+    assert (err <= tol).all(), "%s: %.3g of the bound" % (name, (err / tol).max())
+    norm = 2.0 ** -8 * np.sqrt((ref ** 2).sum() + squares.sum()) + np.sqrt((fp32 ** 2).sum())
+    assert np.sqrt((err ** 2).sum()) <= norm + 1e-30, "%s: %.3g of the norm" % (name, np.sqrt((err ** 2).sum()) / norm)
+
+
+def check_backward(q, k, v, do, m, block, scale, o, lse, got, heads, ordinary=True):
+    pooled = []
+    dq, dk, dv = (bits(x).astype(np.float64) for x in got)
+    group = q.shape[1] // k.shape[1]
+    size = abs(scale)                          # the bounds are of magnitudes
+    f = lambda x: np.asarray(x, dtype=np.float64)
+    for bi in range(q.shape[0]):
+        for hk in sorted({hi // group for hi in heads}):
+            kh, vh = f(k[bi, hk]), f(v[bi, hk])
+            total = [np.zeros_like(kh) for _ in range(8)]
+            exact = [np.zeros_like(kh) for _ in range(2)]
+            for hi in range(hk * group, hk * group + group):
+                qh, gh, oh, lh = f(q[bi, hi]), f(do[bi, hi]), f(o[bi, hi]), f(lse[bi, hi])
+                plain = selection.map_attention_grad(gh, qh, kh, vh, m[bi, hi], block, scale)
+                qk = f(gu.kernel_q(qh, scale))
+                rq, rk, rv = selection.map_attention_grad(gh, qk, kh, vh, m[bi, hi], block, gu.LN2, oh, lh)
+                rq = rq * (scale / gu.LN2)
+                mask = selection._token_mask(m[bi, hi], block, len(qh), len(kh))
+                with np.errstate(over="ignore", invalid="ignore"):
+                    p = np.where(mask, np.exp(gu.LN2 * (qk @ kh.T) - lh[:, None]), 0.0)
+                ds = p * (gh @ vh.T - (gh * oh).sum(1)[:, None])
+                f32 = 2.0 ** -16 * p * (np.abs(gh) @ np.abs(vh).T + (np.abs(gh) * np.abs(oh)).sum(1)[:, None])
+                es, fs = 2.0 ** -8 * np.abs(ds) + f32, f32
+                exact[0] += plain[1]
+                exact[1] += plain[2]
+                if hi in heads:
+                    pooled.append((dq[bi, hi], plain[0]))
+                    near(dq[bi, hi], rq, size * (es @ np.abs(kh)), size * (fs @ np.abs(kh)),
+                         scale ** 2 * (ds ** 2 @ kh ** 2), "dq")
+                es, qk = es + 2.0 ** -8 * np.abs(ds), gu.LN2 * np.abs(qk)
+                parts = (rk, es.T @ qk, fs.T @ qk, 2 * (ds ** 2).T @ qk ** 2,
+                         rv, (2.0 ** -8 + 2.0 ** -16) * (p.T @ np.abs(gh)), 2.0 ** -16 * (p.T @ np.abs(gh)),
+                         (p ** 2).T @ gh ** 2)
+                total = [t + x for t, x in zip(total, parts)]
+            near(dk[bi, hk], *total[:4], "dk")
+            near(dv[bi, hk], *total[4:], "dv")
+            pooled += [(dk[bi, hk], exact[0]), (dv[bi, hk], exact[1])]
+    if ordinary:
+        num, den = sum(((a - b) ** 2).sum() for a, b in pooled), sum((b ** 2).sum() for _, b in pooled)
+        assert num <= gu.REL_L2_TOL ** 2 * den
+
+
+def check(b, h, hk, n_q, n_k, block, d, density=0.4, scale=None, heads=None, seed=0, m=None, data=None, ordinary=True):
+    torch = gu.torch()
+    print(b, h, hk, n_q, n_k, block, d, density, flush=True)
+    q, k, v, do = inputs(seed, b, h, hk, n_q, n_k, d) if data is None else data
+    m = random_map(seed + 1, b, h, blocks(n_q, block), blocks(n_k, block), density) if m is None else m
+    s = d ** -0.5 if scale is None else scale
+    dm = torch.from_numpy(m).to("cuda:0")
+    t = [dev(x) for x in (q, k, v, do)]
+    o, lse = psa.attention_map_fwd(t[0], t[1], t[2], dm, block, scale, return_lse=True)
+    torch.cuda.synchronize()
+    heads = range(h) if heads is None else heads
+    on, ln = bits(o), lse.cpu().numpy()
+    check_forward(q, k, v, m, block, s, on, ln, heads, ordinary)
+    got = psa.attention_map_bwd(t[3], t[0], t[1], t[2], o, lse, dm, block, scale)
+    torch.cuda.synchronize()
+    check_backward(q, k, v, do, m, block, s, on, ln, got, heads, ordinary)
+
+
+SHAPES = [(64, 64), (64, 128), (128, 64), (128, 128)]           # head dim, block
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
+@pytest.mark.parametrize("n_q,n_k", [(1, 1), (1, 64), (1, 700), (3, 129), (33, 1000), (64, 64), (65, 63), (127, 300),
+                                     (128, 128), (129, 257), (500, 500), (700, 90), (1030, 1030)])
+def test_few_query_blocks(d, block, n_q, n_k):
+    """Lists shared out over several workgroups wherever they have two blocks."""
+    check(1, 2, 2, n_q, n_k, block, d)
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
+def test_one_workgroup_per_query_block(d, block):
+    check(2, 40, 40, 4 * block + 17, 5 * block + 1, block, d, heads=[0, 23, 39])
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
+@pytest.mark.parametrize("h,hk", [(4, 2), (6, 1), (8, 8)])
+def test_shared_key_heads(d, block, h, hk):
+    check(2, h, hk, 300, 450, block, d)
+    check(1, 33 * h, 33 * hk, 3 * block, 200, block, d, heads=[0, h, 32 * h + 1])
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
+@pytest.mark.parametrize("density", [0.0, 1.0])
+def test_empty_and_full_maps(d, block, density):
+    nq, nk = 4, 6
+    m = np.full((1, 2, nq, nk), int(density), np.uint8)
+    check(1, 2, 1, nq * block - 3, nk * block - 7, block, d, m=m)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1.0, -0.3, 4.0])
+def test_scales(scale):
+    """Scores from all equal to so far apart that a row has one key (the forward's bar holds for scores of a
+    size that its operand's rounding leaves alone)."""
+    if abs(scale) < 1:
+        check(1, 2, 2, 200, 333, 64, 64, scale=scale)
+    data = inputs(5, 1, 2, 2, 200, 333, 64)
+    torch = gu.torch()
+    m = random_map(6, 1, 2, 4, 6, 0.5)
+    t = [dev(x) for x in data]
+    o, lse = psa.attention_map_fwd(*t[:3], torch.from_numpy(m).to("cuda:0"), 64, scale, return_lse=True)
+    got = psa.attention_map_bwd(t[3], *t[:3], o, lse, torch.from_numpy(m).to("cuda:0"), 64, scale)
+    assert all(torch.isfinite(x).all() for x in (o,) + got)
+
+
+def test_whole_ranges_of_scores():
+    """Rows whose scores sit far from 0, and one key that takes all the weight."""
+    q, k, v, do = inputs(7, 1, 2, 2, 150, 400, 128)
+    q, k = q * 0.25, k.copy()
+    q[..., 0] = 16.0
+    k[:, 0, :, 0] = 100.0
+    k[:, 1, :, 0] = -100.0
+    k[:, :, 77, 1:] = bf16_round(8 * q[:, :, 5, 1:])
+    check(1, 2, 2, 150, 400, 64, 128, density=0.7, data=(bf16_round(q), bf16_round(k), v, do),
+          ordinary=False)
+
+
+def test_gradients_are_differences():
+    """The oracle's loss changes by the kernel's gradients: a step in a random direction against <gradient, step>.
+    The gradients' error is at most 2^-7 of their terms' magnitudes, which the tolerance takes."""
+    torch = gu.torch()
+    b, h, hk, n_q, n_k, d, block = 1, 2, 1, 130, 200, 64, 64
+    q, k, v, do = inputs(11, b, h, hk, n_q, n_k, d)
+    m = random_map(12, b, h, 3, 4, 0.6)
+    t = [dev(x) for x in (q, k, v, do)]
+    dm = torch.from_numpy(m).to("cuda:0")
+    o, lse = psa.attention_map_fwd(*t[:3], dm, block, return_lse=True)
+    grads = [bits(x).astype(np.float64) for x in psa.attention_map_bwd(t[3], *t[:3], o, lse, dm, block)]
+    rng = np.random.default_rng(13)
+    f = [np.asarray(x, dtype=np.float64) for x in (q, k, v)]
+
+    def loss(x):
+        return sum((do[0, i] * selection.map_attention(x[0][0, i], x[1][0, 0], x[2][0, 0], m[0, i], block, d ** -0.5)[0]).sum()
+                   for i in range(h))
+
+    for i in range(3):
+        step = rng.standard_normal(f[i].shape)
+        at = [[x + (s * 1e-4 * step if j == i else 0) for j, x in enumerate(f)] for s in (1, -1)]
+        diff = (loss(at[0]) - loss(at[1])) / 2e-4
+        want = (grads[i] * step).sum()
+        assert abs(diff - want) <= 2.0 ** -7 * np.sqrt((grads[i] ** 2 * step ** 2).sum()) * 4 + 1e-3 * abs(diff)
+
+
+def test_stripes_through_a_map_equal_the_striped_attention():
+    torch = gu.torch()
+    grid, block, heads = (4, 16, 24, 40), 128, 3
+    params = [(1, 0, INF, 2, 0, INF), (2, 1, 3, 1, 0, INF), (4, 0, INF, 1, -1, 3)]
+    n = 4 * 16 * 24 + 40
+    q, k, v, do = inputs(21, 2, heads, heads, n, n, 128)
+    t = [dev(x) for x in (q, k, v)]
+    ref, rl = psa.attention_fwd(*t, grid, block, params, return_lse=True)
+    m, _, _ = psa.build_blockmap(params, grid, block)
+    got, gl = psa.attention_map_fwd(*t, m, block, return_lse=True)     # [heads, nb, nb]: every batch element
+    again = psa.attention_map_fwd(*t, m[None].expand(2, -1, -1, -1).bool(), block)
+    assert torch.equal(again, got)
+    assert (got.float() - ref.float()).norm() <= 1e-2 * ref.float().norm()
+    fin = torch.isfinite(rl)
+    assert torch.equal(fin, torch.isfinite(gl)) and (gl[fin] - rl[fin]).abs().max() <= 2 * gu.LSE_ABS_TOL
+    check_forward(q, k, v, np.broadcast_to(m.cpu().numpy(), (2,) + tuple(m.shape)), block, 128 ** -0.5, bits(got),
+                  gl.cpu().numpy(), range(heads))
+
+
+def test_part_of_a_cache_and_given_outputs():
+    torch = gu.torch()
+    q = torch.randn(2, 4, 70, 128, device="cuda:0").bfloat16()
+    kc, vc = (torch.full((2, 2, 900, 128), float("nan"), device="cuda:0").bfloat16() for _ in range(2))
+    kc[:, :, :333], vc[:, :, :333] = torch.randn(2, 2, 2, 333, 128, device="cuda:0").bfloat16()
+    k, v = kc[:, :, :333], vc[:, :, :333]
+    m = torch.from_numpy(random_map(3, 2, 4, 2, 6, 0.5)).to("cuda:0")
+    ref, rl = psa.attention_map_fwd(q, k.contiguous(), v.contiguous(), m, 64, return_lse=True)
+    room = torch.full((2 * 4 * 70 + 2, 128), 7.0, device="cuda:0").bfloat16()
+    out = room[1:-1].view(2, 4, 70, 128)
+    o, lse = psa.attention_map_fwd(q, k, v, m, 64, return_lse=True, out=out)
+    assert o is out and torch.equal(o, ref) and torch.equal(lse, rl) and (room[0] == 7).all() and (room[-1] == 7).all()
+    do = torch.randn_like(q)
+    g1 = psa.attention_map_bwd(do, q, k, v, o, lse, m, 64)
+    g2 = psa.attention_map_bwd(do, q, k.contiguous(), v.contiguous(), o.clone(), lse, m, 64)
+    assert all(torch.equal(a, b) and torch.isfinite(a).all() for a, b in zip(g1, g2))
+
+
+def test_offsets_past_32_bits():
+    """Key heads more than 2^32 elements apart."""
+    torch = gu.torch()
+    far = 2 ** 32 + 8 * 1000
+    store = torch.empty(far + 200 * 64, dtype=torch.bfloat16, device="cuda:0")
+    k = store.as_strided((1, 2, 200, 64), (0, far, 64, 1))
+    data = torch.randn(2, 200, 64, device="cuda:0").bfloat16()
+    k[0, 0], k[0, 1] = data[0], data[1]
+    q, do = (torch.randn(1, 4, 90, 64, device="cuda:0").bfloat16() for _ in range(2))
+    m = torch.ones(4, 2, 4, dtype=torch.uint8, device="cuda:0")
+    kc = k.contiguous()
+    ref, rl = psa.attention_map_fwd(q, kc, kc, m, 64, return_lse=True)
+    o, lse = psa.attention_map_fwd(q, k, k, m, 64, return_lse=True)
+    assert torch.equal(o, ref) and torch.equal(lse, rl)
+    assert all(torch.equal(a, b) for a, b in zip(psa.attention_map_bwd(do, q, k, k, o, lse, m, 64),
+                                                 psa.attention_map_bwd(do, q, kc, kc, o, lse, m, 64)))
+    assert torch.equal(psa.select_blocks(q, k, 64, 2)[0], psa.select_blocks(q, kc, 64, 2)[0])
+
+
+def test_longest_maps():
+    """7936 blocks on either side, and one more refused."""
+    torch = gu.torch()
+    n = 7936 * 64
+    long, short = torch.randn(1, 1, n, 64, device="cuda:0").bfloat16(), torch.randn(1, 1, 100, 64, device="cuda:0").bfloat16()
+    m, kept = psa.select_blocks(short, long, 64, 33)
+    assert (kept == 33).all() and (m.sum(3) == 33).all()
+    o, lse = psa.attention_map_fwd(short, long, long, m, 64, return_lse=True)
+    mn = m[0, 0].cpu().numpy()
+    at = np.unique(np.nonzero(mn)[1])
+    rows = (at[:, None] * 64 + np.arange(64)).reshape(-1)          # the kept blocks alone are the same attention
+    sub = long[0, 0, torch.from_numpy(rows).to("cuda:0")].float().cpu().numpy()
+    check_forward(bits(short), sub[None, None], sub[None, None], mn[None, None][..., at], 64, 0.125, bits(o), lse.cpu().numpy(), [0])
+    mt = m.transpose(2, 3).contiguous()
+    o, lse = psa.attention_map_fwd(long, short, short, mt, 64, return_lse=True)
+    g = psa.attention_map_bwd(long, long, short, short, o, lse, mt, 64)
+    rest = torch.ones(7936, dtype=torch.bool, device="cuda:0")
+    rest[torch.from_numpy(at).to("cuda:0")] = False
+    empty = o.view(7936, 64, 64)[rest]
+    assert not empty.any() and torch.isneginf(lse.view(7936, 64)[rest]).all() and not g[0].view(7936, 64, 64)[rest].any()
+    few = sub[None, None]
+    check_backward(few, bits(short), bits(short), few, mt.cpu().numpy()[:, :, at], 64, 0.125,
+                   bits(o).reshape(7936, 64, 64)[at].reshape(1, 1, -1, 64), lse.cpu().numpy().reshape(7936, 64)[at].reshape(1, 1, -1),
+                   (g[0].view(7936, 64, 64)[torch.from_numpy(at).to("cuda:0")].view(1, 1, -1, 64), g[1], g[2]), [0])
+    with pytest.raises(psa.PsaError):
+        psa.attention_map_fwd(short, torch.empty(1, 1, n + 1, 64, device="cuda:0", dtype=torch.bfloat16),
+                              torch.empty(1, 1, n + 1, 64, device="cuda:0", dtype=torch.bfloat16),
+                              torch.zeros(1, 2, 7937, dtype=torch.uint8, device="cuda:0"), 64)
+
+
+def test_refusals():
+    torch = gu.torch()
+    q, k = torch.randn(2, 4, 100, 64, device="cuda:0").bfloat16(), torch.randn(2, 2, 150, 64, device="cuda:0").bfloat16()
+    m = torch.ones(2, 4, 2, 3, dtype=torch.uint8, device="cuda:0")
+    lse = torch.zeros(2, 4, 100, device="cuda:0")
+    fwd = lambda **o: psa.attention_map_fwd(**dict(dict(q=q, k=k, v=k, blockmap=m, block=64), **o))
+    bwd = lambda **o: psa.attention_map_bwd(**dict(dict(do=q, q=q, k=k, v=k, o=q, lse=lse, blockmap=m, block=64), **o))
+    for call in (fwd, bwd):
+        for bad in (dict(v=k[:, :, :149]), dict(v=k.float()), dict(blockmap=m[..., :2]), dict(blockmap=m.int()), dict(q=q.cpu()),
+                    dict(blockmap=m.transpose(2, 3).contiguous().transpose(2, 3)), dict(k=k[..., ::2], v=k[..., ::2]),
+                    dict(k=k[:1], v=k[:1]), dict(block=0), dict(q=q[:, :, ::2])):
+            with pytest.raises((ValueError, TypeError)):
+                call(**bad)
+        for bad in (dict(block=32, blockmap=torch.ones(4, 4, 5, dtype=torch.uint8, device="cuda:0")),
+                    dict(k=k[:, :1].repeat(1, 3, 1, 1), v=k[:, :1].repeat(1, 3, 1, 1))):
+            with pytest.raises(psa.PsaError):
+                call(**bad)
+    with pytest.raises(TypeError):
+        fwd(out=q.float())
+    for bad in (dict(lse=lse[:, :, :99]), dict(lse=lse.half()), dict(dk=q), dict(do=q[:, :2].contiguous())):
+        with pytest.raises(ValueError):
+            bwd(**bad)
+    with pytest.raises(psa.PsaError):
+        bwd(workspace=torch.empty(256, dtype=torch.uint8, device="cuda:0"))
+    with pytest.raises(psa.PsaError):        # two query blocks share their lists out
+        fwd(q=q[:1, :1], k=k[:1, :1].repeat(1, 1, 9, 1), v=k[:1, :1].repeat(1, 1, 9, 1),
+            blockmap=torch.ones(1, 2, 22, dtype=torch.uint8, device="cuda:0"),
+            workspace=torch.empty(256, dtype=torch.uint8, device="cuda:0"))
+
+
+def test_together_on_a_side_stream_and_in_a_graph():
+    """A layer as it is used: norm and rotation, selection, attention over the map, and all the gradients back to
+    the projections; eager, on another stream, and captured and replayed on new inputs."""
+    torch = gu.torch()
+    grid, axes, block = (3, 16, 20, 50), (44, 42, 42), 128
+    n = 3 * 16 * 20 + 50
+    xq, xk, xv = (torch.randn(2, n, h, 128, device="cuda:0").bfloat16().transpose(1, 2) for h in (6, 3, 3))
+    wq, wk = (1 + 0.2 * torch.randn(128, device="cuda:0") for _ in range(2))
+    do = torch.randn(2, 6, n, 128, device="cuda:0").bfloat16()
+
+    def layer(stream=None):
+        q, k = psa.qk_norm_rope(xq, xk, grid, axes, q_weight=wq, k_weight=wk, stream=stream)
+        with torch.cuda.stream(stream or torch.cuda.current_stream()):
+            v = xv.contiguous()
+        m, kept = psa.select_blocks(q, k, block, 3, q_text=50, k_text=50, stream=stream)
+        o, lse = psa.attention_map_fwd(q, k, v, m, block, return_lse=True, stream=stream)
+        dq, dk, dv = psa.attention_map_bwd(do, q, k, v, o, lse, m, block, stream=stream)
+        g = psa.qk_norm_rope_bwd(dq, dk, xq, xk, grid, axes, q_weight=wq, k_weight=wk, stream=stream)
+        return (q, k, m, kept, o, lse, dq, dk, dv) + g
+
+    ref = layer()
+    torch.cuda.synchronize()
+    qn, kn, vn = bits(ref[0]), bits(ref[1]), bits(xv)
+    mn = ref[2].cpu().numpy()
+    for hi in range(6):
+        assert np.array_equal(mn[1, hi], selection.select_blocks(qn[1, hi], kn[1, hi // 2], block, 3, 50, 50))
+    check_forward(qn, kn, vn, mn, block, 128 ** -0.5, bits(ref[4]), ref[5].cpu().numpy(), [0, 5])
+    check_backward(qn, kn, vn, bits(do), mn, block, 128 ** -0.5, bits(ref[4]), ref[5].cpu().numpy(), ref[6:9], [0, 5])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = layer(side)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = layer()
+    for replay in range(3):
+        if replay == 2:
+            xq.copy_(torch.randn_like(xq))
+            do.copy_(torch.randn_like(do))
+            ref = layer()
+        for t in got:
+            t.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))

@@ -60,3 +60,66 @@ def test_norm_rope_workspace_size():
     assert size(1, 12, 12, 128, g, 1) >= 2 * 128 * 4 and size(1, 12, 0, 128, g, 1) > 0
     assert size(1, 12, 12, 128, g, 0) == size(0, 12, 12, 128, g, 1) == size(1, 0, 1, 128, g, 1) == 0
     assert size(1, 12, 12, 96, g, 1) == size(1, 12, 12, 64, _lib.grid_of(0, 1, 1), 1) == 0
+
+
+def kv(k=256, v=256, b=2048, h=1024, heads=2):
+    return _lib.Kv(k, v, b, h, heads)
+
+
+def select(q=256, x=kv(), batch=1, heads=4, d=64, n_q=100, n_k=200, block=64, keep=2, qt=0, kt=0, m=1, kept=0, ws=256,
+           wsb=1 << 24):
+    return _lib.lib().psa_select_blocks(vp(q), x, batch, heads, d, n_q, n_k, block, keep, qt, kt, vp(m), vp(kept), vp(ws),
+                                        wsb, None)
+
+
+def mapped(q=256, x=kv(), o=256, batch=1, heads=4, d=64, n_q=100, n_k=2000, block=64, m=1, ms=0, lse=0, ws=256, wsb=1 << 24):
+    return _lib.lib().psa_attention_map_fwd(vp(q), x, vp(o), batch, heads, d, n_q, n_k, block, vp(m), ms, 0.1, vp(lse),
+                                            vp(ws), wsb, None)
+
+
+def mapped_bwd(go=256, q=256, x=kv(), o=256, lse=256, batch=1, heads=4, d=64, n_q=100, n_k=2000, block=64, m=1, ms=0, dq=256,
+               dk=256, dv=256, ws=256, wsb=1 << 24):
+    return _lib.lib().psa_attention_map_bwd(vp(go), vp(q), x, vp(o), vp(lse), batch, heads, d, n_q, n_k, block, vp(m), ms, 0.1,
+                                            vp(dq), vp(dk), vp(dv), vp(ws), wsb, None)
+
+
+SHARED = [(INVALID, dict(q=0)), (INVALID, dict(q=264)), (INVALID, dict(x=None)), (INVALID, dict(x=kv(k=0))),
+          (INVALID, dict(x=kv(k=8))), (INVALID, dict(x=kv(b=4))), (INVALID, dict(x=kv(h=-8))), (INVALID, dict(x=kv(heads=0))),
+          (INVALID, dict(x=kv(heads=3))), (INVALID, dict(x=kv(heads=8))), (INVALID, dict(batch=0)), (INVALID, dict(heads=0)),
+          (UNSUPPORTED, dict(d=96)), (UNSUPPORTED, dict(block=32)), (INVALID, dict(n_q=0)), (INVALID, dict(n_k=0)),
+          (UNSUPPORTED, dict(n_k=7936 * 64 + 1)), (UNSUPPORTED, dict(n_q=7936 * 64 + 1)),
+          (UNSUPPORTED, dict(batch=1 << 20, heads=1 << 10, n_q=1)), (INVALID, dict(m=0)), (WORKSPACE, dict(ws=0)),
+          (WORKSPACE, dict(ws=128)), (WORKSPACE, dict(wsb=16))]
+
+
+@pytest.mark.parametrize("status,bad", SHARED + [
+    (INVALID, dict(keep=-1)), (INVALID, dict(qt=101)), (INVALID, dict(kt=-1)), (INVALID, dict(kt=201)), (INVALID, dict(kept=2))])
+def test_select_refusals(status, bad):
+    assert select(**bad) == status
+    assert _lib.lib().psa_last_error()
+
+
+@pytest.mark.parametrize("status,bad", SHARED + [
+    (INVALID, dict(o=0)), (INVALID, dict(o=8)), (INVALID, dict(x=kv(v=0))), (INVALID, dict(x=kv(v=260))),
+    (INVALID, dict(lse=2)), (INVALID, dict(ms=-1))])
+def test_map_refusals(status, bad):
+    assert mapped(**bad) == status
+
+
+@pytest.mark.parametrize("status,bad", SHARED + [
+    (INVALID, dict(go=0)), (INVALID, dict(go=8)), (INVALID, dict(o=0)), (INVALID, dict(lse=0)), (INVALID, dict(lse=2)),
+    (INVALID, dict(dq=0)), (INVALID, dict(dk=4)), (INVALID, dict(dv=0)), (INVALID, dict(x=kv(v=0)))])
+def test_map_bwd_refusals(status, bad):
+    assert mapped_bwd(**bad) == status
+
+
+def test_workspace_sizes():
+    L = _lib.lib()
+    assert L.psa_select_workspace_size(1, 40, 40, 128, 75600, 75600, 128) >= 2 * 40 * 591 * 128 * 8
+    assert L.psa_select_workspace_size(1, 40, 3, 128, 75600, 75600, 128) == 0
+    assert L.psa_select_workspace_size(0, 40, 40, 128, 75600, 75600, 128) == 0
+    assert L.psa_attention_map_workspace_size(1, 40, 128, 75600, 75600, 128) == 0       # every CU has query blocks
+    assert L.psa_attention_map_workspace_size(1, 4, 128, 1, 75600, 128) > 0
+    assert L.psa_attention_map_workspace_size(1, 4, 100, 1, 75600, 128) == 0
+    assert L.psa_attention_map_bwd_workspace_size(2, 3, 64, 65, 64) >= 2 * 4 * 2 * 3 * 128 + 2 * 6 * 65 * 64
+    assert L.psa_attention_map_bwd_workspace_size(2, 3, 64, 65, 32) == 0
