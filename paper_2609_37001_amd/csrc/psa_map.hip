@@ -63,33 +63,49 @@ __device__ __forceinline__ int32_t item_of(int32_t blk, int32_t items) {
   return at < share && i < items ? i : -1;
 }
 
-// One 32 x 32 tile X Y^T: rows k0 .. k0 + 31 of the tile X in LDS (in the order of key_perm), this lane's row of Y
+// Where this lane reads a tile of rows of D channels in LDS, in bytes from the tile's start: `rows` for the operand of
+// rows_times, `lo` and `hi` for the two halves of cols_times'.  The swizzle is an exclusive or, so the address of
+// a later chunk is that of the first one with bits flipped: one instruction a read.  here() hides the sum
+// with the tile's address from the compiler, which would otherwise keep every flipped address of both
+// buffers in registers across the loop over the blocks (116 of them, spilled: dk and dv of 12 heads x 32760 took
+// 9.5 ms so).
+template <int D>
+struct LaneAt {
+  uint32_t rows, lo, hi;
+  __device__ __forceinline__ explicit LaneAt(int lane) {
+    constexpr int CPR = D / 8, RB = 2 * D;
+    const int h = lane >> 5, g = lane >> 4, j16 = lane & 15;
+    const int kr = key_perm(lane & 31);
+    rows = kr * RB + ((h ^ swz<CPR>(kr)) << 4);
+    const int row = 8 * h + (j16 >> 2), dd = 16 * (g & 1) + 4 * (j16 & 3);
+    lo = row * RB + (((dd >> 3) ^ swz<CPR>(row)) << 4) + (dd & 7) * 2;
+    hi = (row + 4) * RB + (((dd >> 3) ^ swz<CPR>(row + 4)) << 4) + (dd & 7) * 2;
+  }
+  __device__ __forceinline__ static uint32_t here(uint32_t tile, uint32_t lane_at) {
+    uint32_t at = tile + lane_at;
+    asm volatile("" : "+v"(at));
+    return at;
+  }
+};
+
+// One 32 x 32 tile X Y^T: 32 rows of the tile X in LDS from `at` on (in the order of key_perm), this lane's row of Y
 // in registers; acc is where the sums start.
 template <int D>
-__device__ __forceinline__ f32x16 rows_times(const bf16x8 (&y)[D / 16], const uint8_t* x, int k0, int lane, f32x16 acc) {
-  constexpr int CPR = D / 8, RB = 2 * D, DC = D / 16;
-  const int h = lane >> 5, row = k0 + key_perm(lane & 31), sw = swz<CPR>(row);
-  const uint8_t* base = x + row * RB;
+__device__ __forceinline__ f32x16 rows_times(const bf16x8 (&y)[D / 16], uint32_t at, f32x16 acc) {
 #pragma unroll
-  for (int cc = 0; cc < DC; cc++)
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(base + (((2 * cc + h) ^ sw) << 4)), y[cc], acc, 0, 0, 0);
+  for (int cc = 0; cc < D / 16; cc++)
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(PSA_LDS const bf16x8*)(uintptr_t)(at ^ (cc << 5)), y[cc], acc, 0, 0, 0);
   return acc;
 }
 
-// out^T += X^T p for the 16 rows k0 .. k0 + 15 of the tile X in LDS; p holds this lane's eight of them.
+// out^T += X^T p for 16 rows of the tile X in LDS from `lo` and `hi` on; p holds this lane's eight of them.
 template <int D>
-__device__ __forceinline__ void cols_times(f32x16 (&out)[D / 32], const uint8_t* x, int k0, bf16x8 p, int lane) {
-  constexpr int CPR = D / 8, RB = 2 * D, DT = D / 32;
-  const int h = lane >> 5, g = lane >> 4, j16 = lane & 15;
-  const int row = k0 + 8 * h + (j16 >> 2);
-  const int sw0 = swz<CPR>(row), sw1 = swz<CPR>(row + 4);
+__device__ __forceinline__ void cols_times(f32x16 (&out)[D / 32], uint32_t lo, uint32_t hi, bf16x8 p) {
 #pragma unroll
-  for (int dt = 0; dt < DT; dt++) {
-    const int dd = dt * 32 + 16 * (g & 1) + 4 * (j16 & 3);
-    const int chunk = dd >> 3, inoff = (dd & 7) * 2;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PSA_LDS s16x4*)(x + row * RB + ((chunk ^ sw0) << 4) + inoff));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PSA_LDS s16x4*)(x + (row + 4) * RB + ((chunk ^ sw1) << 4) + inoff));
-    const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  for (int dt = 0; dt < D / 32; dt++) {
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PSA_LDS s16x4*)(uintptr_t)(lo ^ (dt << 6)));
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PSA_LDS s16x4*)(uintptr_t)(hi ^ (dt << 6)));
+    const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     out[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p, out[dt], 0, 0, 0);
   }
 }
@@ -349,6 +365,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
     issue_block<D, BLK>(plan, kh, lds_address(sk[0]), kb, n);
     issue_block<D, BLK>(plan, vh, lds_address(sv[0]), kb, n);
   }
+  const LaneAt<D> at_lane(lane);
   bf16x8 q[T::DC], g[T::DC];
   const int64_t at = ((int64_t)bh * n_q + min(row, n_q - 1)) * D;
   load_rows<D>(q, a.q_scaled + at, h);
@@ -370,11 +387,14 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
       issue_block<D, BLK>(plan, kh, lds_address(sk[(i + 1) & 1]), kb, n);
       issue_block<D, BLK>(plan, vh, lds_address(sv[(i + 1) & 1]), kb, n);
     }
+    const uint32_t tk = lds_address(sk[i & 1]) + grp * HK * T::RB, tv = lds_address(sv[i & 1]) + grp * HK * T::RB;
+    const uint32_t kr = LaneAt<D>::here(tk, at_lane.rows), vr = LaneAt<D>::here(tv, at_lane.rows);
+    const uint32_t klo = LaneAt<D>::here(tk, at_lane.lo), khi = LaneAt<D>::here(tk, at_lane.hi);
 #pragma unroll
     for (int kt = 0; kt < HK / 32; kt++) {
       const int k0 = grp * HK + 32 * kt;
-      f32x16 s = rows_times<D>(q, sk[i & 1], k0, lane, (f32x16){} + neg_lse2);
-      f32x16 dp = rows_times<D>(g, sv[i & 1], k0, lane, (f32x16){} + neg_delta);
+      f32x16 s = rows_times<D>(q, kr + 32 * kt * T::RB, (f32x16){} + neg_lse2);
+      f32x16 dp = rows_times<D>(g, vr + 32 * kt * T::RB, (f32x16){} + neg_delta);
       if (tail) {
         // Keys behind the last one read as the last one, whose weight is finite: no gradient of theirs.
         asm volatile("" ::: "memory");        // keep the mask a branch taken only by the last block
@@ -386,7 +406,10 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
       for (int e = 0; e < 16; e++) dp[e] *= __builtin_amdgcn_exp2f(s[e]);
 #pragma unroll
-      for (int j = 0; j < 2; j++) cols_times<D>(dq, sk[i & 1], k0 + 16 * j, half_of(dp, j), lane);
+      for (int j = 0; j < 2; j++) {
+        const int off = (32 * kt + 16 * j) * T::RB;
+        cols_times<D>(dq, klo + off, khi + off, half_of(dp, j));
+      }
     }
   }
 
@@ -449,6 +472,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   for (int dt = 0; dt < T::DT; dt++) dk[dt] = dv[dt] = (f32x16){};
   DmaPlan<D, BLK> plan;
   plan.init(__builtin_amdgcn_readfirstlane(wave), lane);
+  const LaneAt<D> at_lane(lane);
 
   for (int32_t hd = hk * a.group; hd < (hk + 1) * a.group; hd++) {
     const int64_t bh = (int64_t)b * a.n_heads + hd;
@@ -476,27 +500,32 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
       __syncthreads();
       const bool more = i + 1 < nu;
       if (more) issue(i + 1);
-      const uint8_t *tq = sq[i & 1], *tg = sg[i & 1];
+      const uint32_t tq = lds_address(sq[i & 1]) + grp * HQ * T::RB, tg = lds_address(sg[i & 1]) + grp * HQ * T::RB;
+      const uint32_t qr = LaneAt<D>::here(tq, at_lane.rows), gr = LaneAt<D>::here(tg, at_lane.rows);
+      const uint32_t qlo = LaneAt<D>::here(tq, at_lane.lo), qhi = LaneAt<D>::here(tq, at_lane.hi);
+      const uint32_t glo = LaneAt<D>::here(tg, at_lane.lo), ghi = LaneAt<D>::here(tg, at_lane.hi);
 #pragma unroll
       for (int kt = 0; kt < HQ / 32; kt++) {
         const int q0 = grp * HQ + 32 * kt;
-        f32x16 s = rows_times<D>(k, tq, q0, lane, start_of(&stat[i & 1][0][q0 + 8 * h]));
+        f32x16 s = rows_times<D>(k, qr + 32 * kt * T::RB, start_of(&stat[i & 1][0][q0 + 8 * h]));
         bf16x8 p[2];
 #pragma unroll
         for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(s[e]);
 #pragma unroll
-        for (int j = 0; j < 2; j++) p[j] = half_of(s, j);
-#pragma unroll
-        for (int j = 0; j < 2; j++) cols_times<D>(dv, tg, q0 + 16 * j, p[j], lane);
-        f32x16 dp = rows_times<D>(v, tg, q0, lane, start_of(&stat[i & 1][1][q0 + 8 * h]));
+        for (int j = 0; j < 2; j++) {
+          const int off = (32 * kt + 16 * j) * T::RB;
+          p[j] = half_of(s, j);
+          cols_times<D>(dv, glo + off, ghi + off, p[j]);
+        }
+        f32x16 dp = rows_times<D>(v, gr + 32 * kt * T::RB, start_of(&stat[i & 1][1][q0 + 8 * h]));
 #pragma unroll
         for (int j = 0; j < 2; j++) {
+          const int off = (32 * kt + 16 * j) * T::RB;
           const f32x8 pf = __builtin_convertvector(p[j], f32x8);
 #pragma unroll
           for (int e = 0; e < 8; e++) dp[8 * j + e] *= pf[e];
+          cols_times<D>(dk, qlo + off, qhi + off, half_of(dp, j));
         }
-#pragma unroll
-        for (int j = 0; j < 2; j++) cols_times<D>(dk, tq, q0 + 16 * j, half_of(dp, j), lane);
       }
       if (more) put(i + 1);
     }
