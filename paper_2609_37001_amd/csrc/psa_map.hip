@@ -508,22 +508,18 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int kt = 0; kt < HQ / 32; kt++) {
         const int q0 = grp * HQ + 32 * kt;
         f32x16 s = rows_times<D>(k, qr + 32 * kt * T::RB, start_of(&stat[i & 1][0][q0 + 8 * h]));
-        bf16x8 p[2];
+        f32x16 dp = rows_times<D>(v, gr + 32 * kt * T::RB, start_of(&stat[i & 1][1][q0 + 8 * h]));
 #pragma unroll
         for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(s[e]);
 #pragma unroll
         for (int j = 0; j < 2; j++) {
           const int off = (32 * kt + 16 * j) * T::RB;
-          p[j] = half_of(s, j);
-          cols_times<D>(dv, glo + off, ghi + off, p[j]);
+          cols_times<D>(dv, glo + off, ghi + off, half_of(s, j));
         }
-        f32x16 dp = rows_times<D>(v, gr + 32 * kt * T::RB, start_of(&stat[i & 1][1][q0 + 8 * h]));
+        dp *= s;
 #pragma unroll
         for (int j = 0; j < 2; j++) {
           const int off = (32 * kt + 16 * j) * T::RB;
-          const f32x8 pf = __builtin_convertvector(p[j], f32x8);
-#pragma unroll
-          for (int e = 0; e < 8; e++) dp[8 * j + e] *= pf[e];
           cols_times<D>(dk, qlo + off, qhi + off, half_of(dp, j));
         }
       }
