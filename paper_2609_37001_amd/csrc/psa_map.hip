@@ -127,6 +127,15 @@ struct Stream {
   }
 };
 
+// Loads 64 words from x on into LDS, one per lane.
+__device__ __forceinline__ void dma4(uint32_t lds, int lane, const void* x) {
+  asm volatile("" : "+v"(lane));          // (the offset is formed here, not kept in a register)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(4 * lane), "s"(x)
+               : "memory");
+}
+
 // One 32 x 32 tile X Y^T: 32 rows of the tile X in LDS from `at` on (in the order of key_perm), this lane's row of Y
 // in registers; acc is where the sums start.
 template <int D>
@@ -509,30 +518,26 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   f32x16 dk[T::DT], dv[T::DT];
 #pragma unroll
   for (int dt = 0; dt < T::DT; dt++) dk[dt] = dv[dt] = (f32x16){};
-  const Stream<D, BLK> stream(__builtin_amdgcn_readfirstlane(wave), lane);
+  const int wave_s = __builtin_amdgcn_readfirstlane(wave);
+  const Stream<D, BLK> stream(wave_s, lane);
   const LaneAt<D> at_lane(lane);
 
   for (int32_t hd = hk * a.group; hd < (hk + 1) * a.group; hd++) {
     const int64_t bh = (int64_t)b * a.n_heads + hd;
     const __bf16 *qh = a.q_scaled + bh * n_q * D, *gh = a.grad_o + bh * n_q * D;
-    const float* sh = (tid < BLK ? a.neg_lse2 : a.neg_delta) + bh * a.nbq * BLK;
+    // This wave's 64 of the 2 BLK row values of a block (waves behind them load none).
+    const int part = wave_s * 64 / BLK, place = wave_s * 64 % BLK;
+    const float* sh = (part == 0 ? a.neg_lse2 : a.neg_delta) + bh * a.nbq * BLK + place;
     // (its barriers also separate the buffers from the head before)
     const int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + (int64_t)hd * a.nbq * a.nbk + kb, a.nbk, a.nbq, list, found);
     auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[i]); };
-    float next = 0.0f;
     auto issue = [&](int i) {
       const int qb = entry(i);
       stream.load(qh, lds_address(sq[i & 1]), qb, n_q);
       stream.load(gh, lds_address(sg[i & 1]), qb, n_q);
-      if (tid < 2 * BLK) next = sh[qb * BLK + (tid & (BLK - 1))];
+      if (part < 2) dma4(lds_address(&stat[i & 1][part][place]), lane, sh + (int64_t)qb * BLK);
     };
-    auto put = [&](int i) {
-      if (tid < 2 * BLK) stat[i & 1][tid / BLK][tid & (BLK - 1)] = next;
-    };
-    if (nu > 0) {
-      issue(0);
-      put(0);
-    }
+    if (nu > 0) issue(0);
     for (int i = 0; i < nu; i++) {
       wait_dma<0>();
       __syncthreads();
@@ -562,7 +567,6 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
           cols_times<D>(dk, qlo + off, qhi + off, half_of(dp, j));
         }
       }
-      if (more) put(i + 1);
     }
   }
 
