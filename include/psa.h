@@ -412,8 +412,9 @@ psa_status_t psa_select_blocks(const void* q, const psa_kv_t* kv, int32_t batch,
                                int32_t q_text, int32_t k_text, uint8_t* blockmap, int32_t* kept_per_row,
                                void* workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* Bytes of device workspace of psa_attention_map_fwd (0 if invalid, or if none is needed: only calls of few
- * query blocks, whose lists are shared out over several workgroups, need one). */
+/* Bytes of device workspace of psa_attention_map_fwd (0 if invalid, or if none is needed).  Calls of few query
+ * blocks, whose lists are shared out over several workgroups, keep their partial sums there, calls of many the
+ * order in which they are taken, those with the longest lists first. */
 size_t psa_attention_map_workspace_size(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_q,
                                         int32_t n_k, int32_t block);
 
@@ -432,8 +433,8 @@ psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, i
                                    size_t workspace_bytes, hipStream_t stream);
 
 /* Bytes of device workspace of psa_attention_map_bwd (0 if invalid). */
-size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_q,
-                                            int32_t block);
+size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads,
+                                            int32_t head_dim, int32_t n_q, int32_t n_k, int32_t block);
 
 /* Gradients of psa_attention_map_fwd.  Scores are formed again as the forward does (q scaled and rounded to bf16
  * once, also in dk; products summed in fp32), so that the weights are those of its lse; the weights and their

@@ -718,7 +718,7 @@ def attention_map_bwd(do, q, k, v, o, lse, blockmap, block, scale=None, dq=None,
         _check_q(dk, "dk", k)
         _check_q(dv, "dv", k)
         L = _lib.lib()
-        ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_bwd_workspace_size(b, h, d, n_q, int(block))), q.device)
+        ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_bwd_workspace_size(b, h, k.shape[1], d, n_q, n_k, int(block))), q.device)
         _lib.check(L.psa_attention_map_bwd(_ptr(do), _ptr(q), kv, _ptr(o), _ptr(lse), b, h, d, n_q, n_k, int(block), bm,
                                            bm_stride, scale, _ptr(dq), _ptr(dk), _ptr(dv), ws, nbytes,
                                            _stream(None, q.device)))

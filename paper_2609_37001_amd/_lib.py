@@ -156,7 +156,7 @@ def lib():
         L.psa_attention_map_workspace_size.restype = sz
         L.psa_attention_map_fwd.argtypes = [vp, kv, vp] + [i32] * 6 + [vp, i64, ctypes.c_float, vp, vp, sz, vp]
         L.psa_attention_map_fwd.restype = ctypes.c_int
-        L.psa_attention_map_bwd_workspace_size.argtypes = [i32] * 5
+        L.psa_attention_map_bwd_workspace_size.argtypes = [i32] * 7
         L.psa_attention_map_bwd_workspace_size.restype = sz
         L.psa_attention_map_bwd.argtypes = [vp, vp, kv, vp, vp] + [i32] * 6 + [vp, i64, ctypes.c_float, vp, vp, vp,
                                                                               vp, sz, vp]

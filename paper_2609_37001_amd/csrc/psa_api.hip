@@ -819,16 +819,18 @@ psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, i
   a.parts = l.parts;
   a.part_o = (float*)workspace;
   a.part_ml = (float2*)((char*)workspace + l.part_ml);
+  a.row_counts = (int32_t*)workspace;
+  a.row_order = (int32_t*)((char*)workspace + l.order);
   const hipError_t e = psa::launch_map_fwd(a, head_dim, stream);
   return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_attention_map_fwd launch");
 }
 
-size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_q,
-                                            int32_t block) {
+size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                            int32_t n_q, int32_t n_k, int32_t block) {
   const SavedError keep;
   int32_t nbq, nbk;
-  if (check_mapped(batch, n_heads, 1, head_dim, n_q, 1, block, &nbq, &nbk) != PSA_OK) return 0;
-  return psa::map_bwd_layout(batch * n_heads, head_dim, n_q, nbq, block).total;
+  if (check_mapped(batch, n_heads, n_kv_heads, head_dim, n_q, n_k, block, &nbq, &nbk) != PSA_OK) return 0;
+  return psa::map_bwd_layout(batch * n_heads, batch * n_kv_heads, head_dim, n_q, nbq, nbk, block).total;
 }
 
 psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_kv_t* kv, const void* o,
@@ -845,7 +847,7 @@ psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_
   for (const void* p : {grad_o, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!p || !aligned(p, 16))
       return fail(PSA_ERR_INVALID, "grad_o, dq, dk and dv must be non-NULL and 16-byte aligned (%p)", p);
-  const psa::MapBwdLayout l = psa::map_bwd_layout(a.n_bh, head_dim, n_q, a.nbq, block);
+  const psa::MapBwdLayout l = psa::map_bwd_layout(a.n_bh, batch * kv->n_heads, head_dim, n_q, a.nbq, a.nbk, block);
   s = check_map_workspace(workspace, workspace_bytes, l.total);
   if (s != PSA_OK) return s;
   a.grad_o = (const __bf16*)grad_o;
@@ -855,6 +857,10 @@ psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_
   a.q_scaled = (__bf16*)workspace;
   a.neg_lse2 = (float*)((char*)workspace + l.neg_lse2);
   a.neg_delta = (float*)((char*)workspace + l.neg_delta);
+  a.row_counts = (int32_t*)((char*)workspace + l.row_counts);
+  a.row_order = (int32_t*)((char*)workspace + l.row_order);
+  a.col_counts = (int32_t*)((char*)workspace + l.col_counts);
+  a.col_order = (int32_t*)((char*)workspace + l.col_order);
   const hipError_t e = psa::launch_map_bwd(a, head_dim, stream);
   return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_attention_map_bwd launch");
 }

@@ -291,20 +291,23 @@ struct MapArgs {
   float2* part_ml;
   float *neg_lse2, *neg_delta;        // backward: [n_bh][nbq][block]
   __bf16* q_scaled;                   // backward: bf16(scale log2(e) q), like q
+  int32_t *row_counts, *row_order;    // list lengths of the (head, query block) items and their order
+  int32_t *col_counts, *col_order;    // backward: those of the (key head, key block) items
   int32_t n_bh, n_heads, group;       // group: query heads per key head
   int32_t n_q, n_k, nbq, nbk, block, parts;
   float c, scale;                     // scale log2(e), scale
 };
 struct MapLayout {
   int32_t parts;
-  size_t part_ml, total;              // (part_o first)
+  size_t part_ml, order, total;       // part_o first, or, in one part, the items' list lengths
 };
 MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);
 struct MapBwdLayout {
-  size_t neg_lse2, neg_delta, total;  // (q_scaled first)
+  size_t neg_lse2, neg_delta, row_counts, row_order, col_counts, col_order, total;  // (q_scaled first)
 };
-MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t head_dim, int32_t n_q, int32_t nbq, int32_t block);
+MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t n_q, int32_t nbq, int32_t nbk,
+                            int32_t block);
 hipError_t launch_map_bwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);
 
 // Device address of the static scratch of psa_attention_fwd_noalloc on the current device

@@ -55,12 +55,129 @@ __device__ __forceinline__ int32_t kept_list(const uint8_t* __restrict__ row, in
   return __builtin_amdgcn_readfirstlane(nu);
 }
 
-// Workgroup -> item: consecutive workgroups go to the XCDs in turn, so each XCD takes a contiguous range of the
-// items, whose blocks stream much the same other side through its L2.
+// Position j of a run of `len` items -> its place among workgroups that start in turn: consecutive workgroups go to the
+// XCDs in turn, so XCD x gets the x-th contiguous part of the run, whose blocks stream much the same other side
+// through its L2.  (The last len % 8 items follow one by one.)
+__device__ __forceinline__ int32_t spread(int32_t j, int32_t len) {
+  const int32_t part = len / kNumQueues;
+  if (j >= part * kNumQueues) return j;
+  const int32_t x = j / part;
+  return (j - x * part) * kNumQueues + x;
+}
+
+// The reverse: the item that workgroup `blk` of `items` takes.
 __device__ __forceinline__ int32_t item_of(int32_t blk, int32_t items) {
-  const int32_t share = (items + kNumQueues - 1) / kNumQueues;
-  const int32_t at = blk / kNumQueues, i = blk % kNumQueues * share + at;
-  return at < share && i < items ? i : -1;
+  const int32_t part = items / kNumQueues;
+  return blk >= part * kNumQueues ? blk : blk % kNumQueues * part + blk / kNumQueues;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Order of the items: those with long lists first.  Where the items outnumber the workgroups that run at once, a
+// long one that starts late is waited for alone (a row of text, a key block that everybody keeps).  Items whose
+// lists are about as long stay in their order, for the XCDs' sake.
+// ---------------------------------------------------------------------------------------------
+
+// Kept key blocks of every (head, query block), a wave each.
+__global__ __launch_bounds__(256) void psa_mapped_row_count_kernel(MapArgs a) {
+  const int32_t item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (item >= a.n_bh * a.nbq) return;
+  const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
+  const uint8_t* row = a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk;
+  int32_t c = 0;
+#pragma unroll 8
+  for (int32_t j = lane; j < a.nbk; j += 64) c += row[j] != 0;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) c += __shfl_xor(c, off);
+  if (lane == 0) a.row_counts[item] = c;
+}
+
+// Kept (query head, query block) pairs of every (key head, key block); 64 key blocks per workgroup.
+__global__ __launch_bounds__(256) void psa_mapped_col_count_kernel(MapArgs a) {
+  __shared__ int32_t part[4][64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int32_t n_kv = a.n_heads / a.group, per = (a.nbk + 63) / 64, bk = blockIdx.x / per, b = bk / n_kv, hk = bk - b * n_kv;
+  const int32_t kb = (blockIdx.x - bk * per) * 64 + lane;
+  // the rows of a key head's query heads lie one behind the other
+  const uint8_t* col = a.map + b * a.map_stride_b + (int64_t)hk * a.group * a.nbq * a.nbk + min(kb, a.nbk - 1);
+  int32_t c = 0;
+#pragma unroll 8
+  for (int32_t i = wave; i < a.group * a.nbq; i += 4) c += col[(int64_t)i * a.nbk] != 0;
+  part[wave][lane] = c;
+  __syncthreads();
+  if (wave == 0 && kb < a.nbk) a.col_counts[bk * a.nbk + kb] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+}
+
+// order[workgroup] = item: eight classes of list lengths around the mean, longest first, each in the items' order and
+// spread over the XCDs.  One workgroup per list of items (rows, columns); each thread takes a run of them.
+constexpr int kOrderThreads = 1024, kOrderClasses = 8;
+__global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(const int32_t* __restrict__ counts0, int32_t* __restrict__ order0,
+                                                                         int32_t n0, const int32_t* __restrict__ counts1,
+                                                                         int32_t* __restrict__ order1, int32_t n1) {
+  __shared__ int32_t at[kOrderClasses * kOrderThreads];
+  __shared__ int32_t waves[kOrderThreads / 64];
+  __shared__ unsigned long long total;
+  const int32_t* counts = blockIdx.x ? counts1 : counts0;
+  int32_t* order = blockIdx.x ? order1 : order0;
+  const int32_t n = blockIdx.x ? n1 : n0;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int32_t each = (n + kOrderThreads - 1) / kOrderThreads, i0 = min(n, tid * each), i1 = min(n, i0 + each);
+  if (tid == 0) total = 0;
+  __syncthreads();
+  unsigned long long mine = 0;
+  for (int32_t i = i0; i < i1; i++) mine += counts[i];
+  atomicAdd(&total, mine);
+  __syncthreads();
+  const float mean = (float)total / (float)n;
+  auto cls = [&](int32_t c) {
+    const float x = (float)c;
+    return x >= 4.0f * mean ? 0 : x >= 2.83f * mean ? 1 : x >= 2.0f * mean ? 2 : x >= 1.5f * mean ? 3 :
+           x >= 1.25f * mean ? 4 : x >= 1.1f * mean ? 5 : x >= 0.9f * mean ? 6 : 7;
+  };
+  int32_t have[kOrderClasses] = {};
+  for (int32_t i = i0; i < i1; i++) {
+    const int k = cls(counts[i]);
+#pragma unroll
+    for (int x = 0; x < kOrderClasses; x++) have[x] += x == k;
+  }
+#pragma unroll
+  for (int x = 0; x < kOrderClasses; x++) at[x * kOrderThreads + tid] = have[x];
+  __syncthreads();
+  // exclusive sums over (class, thread): eight entries a thread, then over the threads
+  int32_t v[kOrderClasses], sum = 0;
+#pragma unroll
+  for (int x = 0; x < kOrderClasses; x++) {
+    v[x] = sum;
+    sum += at[tid * kOrderClasses + x];
+  }
+  int32_t up = sum;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int32_t y = __shfl_up(up, off);
+    if (lane >= off) up += y;
+  }
+  if (lane == 63) waves[wave] = up;
+  __syncthreads();
+  int32_t before = up - sum;
+  for (int w = 0; w < wave; w++) before += waves[w];
+#pragma unroll
+  for (int x = 0; x < kOrderClasses; x++) at[tid * kOrderClasses + x] = before + v[x];
+  __syncthreads();
+  int32_t next[kOrderClasses], start[kOrderClasses + 1];
+#pragma unroll
+  for (int x = 0; x < kOrderClasses; x++) {
+    next[x] = at[x * kOrderThreads + tid];
+    start[x] = at[x * kOrderThreads];
+  }
+  start[kOrderClasses] = n;
+  for (int32_t i = i0; i < i1; i++) {
+    const int k = cls(counts[i]);
+#pragma unroll
+    for (int x = 0; x < kOrderClasses; x++)
+      if (x == k) {
+        order[start[x] + spread(next[x] - start[x], start[x + 1] - start[x])] = i;
+        next[x]++;
+      }
+  }
 }
 
 // Where this lane reads a tile of rows of D channels in LDS, in bytes from the tile's start: `rows` for the operand of
@@ -205,9 +322,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ float2 stat[W][32];              // (m, l) of every wave's rows
   extern __shared__ uint16_t list[];          // nbk entries
 
-  const int32_t items = a.n_bh * a.nbq * (SPLIT ? a.parts : 1);
-  const int32_t whole = item_of(blockIdx.x, items);
-  if (whole < 0) return;
+  const int32_t whole = a.row_order ? a.row_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
   const int32_t item = SPLIT ? whole / a.parts : whole, part = SPLIT ? whole - item * a.parts : 0;
   const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
@@ -392,8 +507,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ int32_t found[W];
   extern __shared__ uint16_t list[];          // nbk entries
 
-  const int32_t item = item_of(blockIdx.x, a.n_bh * a.nbq);
-  if (item < 0) return;
+  const int32_t item = a.row_order ? a.row_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
   const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
   const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
@@ -500,8 +614,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ int32_t found[W];
   extern __shared__ uint16_t list[];          // nbq entries
 
-  const int32_t item = item_of(blockIdx.x, a.n_bh / a.group * a.nbk);
-  if (item < 0) return;
+  const int32_t item = a.col_order ? a.col_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
   const int32_t bk = item / a.nbk, kb = item - bk * a.nbk, n_kv = a.n_heads / a.group;
   const int32_t b = bk / n_kv, hk = bk - b * n_kv;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
@@ -600,7 +713,10 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
-int32_t grid_of(int32_t items) { return (items + kNumQueues - 1) / kNumQueues * kNumQueues; }
+// Whether the items are more than the workgroups that run at once (one of 128 rows to a CU, two of 64).
+bool ordered(int64_t items, int32_t block) { return items > 256 * (128 / block); }
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 int32_t list_bytes(int32_t nb) { return (2 * nb + 15) & ~15; }
 
@@ -622,36 +738,66 @@ int32_t map_parts(int32_t n_bh, int32_t nbq, int32_t nbk, int32_t block) {
 }
 
 MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
-  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   MapLayout l = {};
   l.parts = map_parts(n_bh, nbq, nbk, block);
+  const size_t items = (size_t)n_bh * nbq, rows = items * l.parts * block;
   if (l.parts > 1) {
-    const size_t rows = (size_t)n_bh * nbq * l.parts * block;
-    l.part_ml = up(rows * head_dim * sizeof(float));
-    l.total = l.part_ml + up(rows * sizeof(float2));
+    l.part_ml = up256(rows * head_dim * sizeof(float));
+    l.total = l.part_ml + up256(rows * sizeof(float2));
+  } else if (ordered(items, block)) {
+    l.order = up256(items * sizeof(int32_t));
+    l.total = 2 * l.order;
   }
   return l;
 }
 
-MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t head_dim, int32_t n_q, int32_t nbq, int32_t block) {
-  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  const size_t rows = up((size_t)n_bh * nbq * block * sizeof(float));
+MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t n_q, int32_t nbq, int32_t nbk,
+                            int32_t block) {
+  const size_t rows = up256((size_t)n_bh * nbq * block * sizeof(float));
+  const size_t q_items = up256((size_t)n_bh * nbq * sizeof(int32_t)), k_items = up256((size_t)n_kv * nbk * sizeof(int32_t));
   MapBwdLayout l;
-  l.neg_lse2 = up((size_t)n_bh * n_q * head_dim * sizeof(__bf16));
+  l.neg_lse2 = up256((size_t)n_bh * n_q * head_dim * sizeof(__bf16));
   l.neg_delta = l.neg_lse2 + rows;
-  l.total = l.neg_delta + rows;
+  l.row_counts = l.neg_delta + rows;
+  l.row_order = l.row_counts + q_items;
+  l.col_counts = l.row_order + q_items;
+  l.col_order = l.col_counts + k_items;
+  l.total = l.col_order + k_items;
   return l;
 }
 
-hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream) {
+// The orders of the rows and columns that outnumber the workgroups; clears the pointers of the others.
+static hipError_t launch_orders(MapArgs& a, bool cols, hipStream_t stream) {
+  const int32_t n0 = a.n_bh * a.nbq, n1 = a.n_bh / a.group * a.nbk;
+  const bool by_row = ordered(n0, a.block), by_col = cols && ordered(n1, a.block);
+  if (!by_row) a.row_order = nullptr;
+  if (!by_col) a.col_order = nullptr;
+  if (!by_row && !by_col) return hipSuccess;
+  if (by_row) hipLaunchKernelGGL(psa_mapped_row_count_kernel, dim3((n0 + 3) / 4), dim3(256), 0, stream, a);
+  if (by_col)
+    hipLaunchKernelGGL(psa_mapped_col_count_kernel, dim3((a.nbk + 63) / 64 * (a.n_bh / a.group)), dim3(256), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int32_t *c0 = by_row ? a.row_counts : a.col_counts, *c1 = a.col_counts;
+  int32_t *o0 = by_row ? a.row_order : a.col_order, *o1 = a.col_order;
+  hipLaunchKernelGGL(psa_mapped_order_kernel, dim3(by_row + by_col), dim3(kOrderThreads), 0, stream, c0, o0, by_row ? n0 : n1,
+                     c1, o1, n1);
+  return hipGetLastError();
+}
+
+hipError_t launch_map_fwd(const MapArgs& args, int32_t head_dim, hipStream_t stream) {
+  MapArgs a = args;
+  hipError_t e = a.parts == 1 ? launch_orders(a, false, stream) : hipSuccess;
+  if (e != hipSuccess) return e;
   return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
     constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
-    const int32_t grid = grid_of(a.n_bh * a.nbq * a.parts);
+    const dim3 grid(a.n_bh * a.nbq * a.parts);
     if (a.parts == 1) {
-      hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, false>), dim3(grid), dim3(4 * B), list_bytes(a.nbk), stream, a);
+      hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, false>), grid, dim3(4 * B), list_bytes(a.nbk), stream, a);
       return hipGetLastError();
     }
-    hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, true>), dim3(grid), dim3(4 * B), list_bytes(a.nbk), stream, a);
+    a.row_order = nullptr;
+    hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, true>), grid, dim3(4 * B), list_bytes(a.nbk), stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t rows = (int64_t)a.n_bh * a.n_q;
@@ -660,19 +806,21 @@ hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream
   });
 }
 
-hipError_t launch_map_bwd(const MapArgs& a, int32_t head_dim, hipStream_t stream) {
+hipError_t launch_map_bwd(const MapArgs& args, int32_t head_dim, hipStream_t stream) {
+  MapArgs a = args;
+  hipError_t e = launch_orders(a, true, stream);
+  if (e != hipSuccess) return e;
   return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
     constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
     const int64_t rows = (int64_t)a.n_bh * a.nbq * B;
     hipLaunchKernelGGL(psa_mapped_rows_kernel<D>, dim3((uint32_t)((rows * (D / 8) + 255) / 256)), dim3(256), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B>), dim3(grid_of(a.n_bh / a.group * a.nbk)), dim3(4 * B),
-                       list_bytes(a.nbq), stream, a);
+    hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B>), dim3(a.n_bh / a.group * a.nbk), dim3(4 * B), list_bytes(a.nbq),
+                       stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B>), dim3(grid_of(a.n_bh * a.nbq)), dim3(4 * B), list_bytes(a.nbk),
-                       stream, a);
+    hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B>), dim3(a.n_bh * a.nbq), dim3(4 * B), list_bytes(a.nbk), stream, a);
     return hipGetLastError();
   });
 }
