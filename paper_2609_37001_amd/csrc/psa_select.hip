@@ -77,22 +77,31 @@ __device__ __forceinline__ uint64_t ordered(double s) {
 
 constexpr int kSelectRows = 16;
 
-// Key blocks whose scores a workgroup keeps in LDS (two workgroups per CU); above, they go to a slab of the
-// workspace, which stays in the L2.  R: score words per lane and row in registers (0: read again for every
-// bit).
-template <int R, bool LDS>
-struct SelectForm {
-  static constexpr int kCap = LDS ? 64 * R - 16 : 1;
-};
+// LDS: the workgroup's scores are kept there, up to kSelectLds key blocks (two workgroups per CU, more where they
+// are fewer).  Else they go to a slab of the workspace, which stays in the L2.  R: score words per lane and row in
+// registers (0: read again for every bit).
+constexpr int kSelectLds = 624;
+
+// The means of 16 blocks as the matrix core's operand: of block j (16 of them over lane % 16) this lane's channels
+// are 8 s + 2 part + {0, 1}, part = lane / 16, at element 4 s.  (Any assignment of channels to the steps of a product
+// will do if both sides share it; this one reads 64 contiguous bytes of a block at a time.)
+template <int D>
+__device__ __forceinline__ const f64x2* mean_of(const double* mean, int32_t j, int32_t nb, int part) {
+  return (const f64x2*)(mean + (int64_t)min(j, nb - 1) * D) + part;
+}
+
+// Eight waves, two workgroups per CU at 624 key blocks: the search is a chain of compares and counts that only other
+// waves can fill.
+constexpr int kSelectWaves = 8;
 
 template <int D, int R, bool LDS>
-__global__ __launch_bounds__(256) void psa_select_kernel(SelectArgs a) {
-  constexpr int S = D / 4;                         // channels of a lane: k = S (lane / 16) + s
-  __shared__ uint64_t keys[LDS ? kSelectRows * SelectForm<R, LDS>::kCap : 1];
+__global__ __launch_bounds__(64 * kSelectWaves) __attribute__((amdgpu_waves_per_eu(4))) void psa_select_kernel(SelectArgs a) {
+  constexpr int S = D / 4;                         // channels of a lane
+  extern __shared__ uint64_t lds_words[];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, part = lane >> 4;
   const int32_t per_head = (a.nbq + kSelectRows - 1) / kSelectRows, items = a.n_bh * per_head;
-  const int32_t cap = LDS ? SelectForm<R, LDS>::kCap : a.slab;
-  uint64_t* const words = LDS ? keys : a.scores + (int64_t)blockIdx.x * kSelectRows * a.slab;
+  const int32_t cap = a.slab;
+  uint64_t* const words = LDS ? lds_words : a.scores + (int64_t)blockIdx.x * kSelectRows * cap;
   // consecutive items of one XCD share the keys' means
   const int32_t share = (items + kNumQueues - 1) / kNumQueues;
   for (int32_t at = blockIdx.x / kNumQueues; at < share; at += gridDim.x / kNumQueues) {
@@ -103,18 +112,19 @@ __global__ __launch_bounds__(256) void psa_select_kernel(SelectArgs a) {
     const int32_t kept = min(a.keep, a.first_k);
     // A row that keeps all or nothing needs no scores.
     if (kept > 0 && kept < a.first_k && i0 < a.first_q) {
-      const double* mq = a.mean_q + ((int64_t)bh * a.nbq + min(i0 + col, a.nbq - 1)) * D + S * part;
-      f64x2 qa[S / 2];
+      const double* mk = a.mean_k + (int64_t)kv * a.nbk * D;
+      const f64x2* mq = mean_of<D>(a.mean_q + (int64_t)bh * a.nbq * D, i0 + col, a.nbq, part);
+      f64x2 q[S / 2];
 #pragma unroll
-      for (int s = 0; s < S / 2; s++) qa[s] = ((const f64x2*)mq)[s];
-      for (int32_t j0 = 16 * wave; j0 < a.first_k; j0 += 64) {
-        const double* mk = a.mean_k + ((int64_t)kv * a.nbk + min(j0 + col, a.nbk - 1)) * D + S * part;
+      for (int s = 0; s < S / 2; s++) q[s] = mq[4 * s];
+      for (int32_t j0 = 16 * wave; j0 < a.first_k; j0 += 16 * kSelectWaves) {
+        const f64x2* k = mean_of<D>(mk, j0 + col, a.nbk, part);
         f64x4 acc = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
         for (int s = 0; s < S / 2; s++) {
-          const f64x2 kb = ((const f64x2*)mk)[s];
-          acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qa[s][0], kb[0], acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qa[s][1], kb[1], acc, 0, 0, 0);
+          const f64x2 x = k[4 * s];
+          acc = __builtin_amdgcn_mfma_f64_16x16x4f64(q[s][0], x[0], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f64_16x16x4f64(q[s][1], x[1], acc, 0, 0, 0);
         }
         // element e: query block 4 e + part, key block col
         if (j0 + col < a.first_k)
@@ -123,7 +133,7 @@ __global__ __launch_bounds__(256) void psa_select_kernel(SelectArgs a) {
       }
       __syncthreads();
     }
-    for (int row = wave; row < kSelectRows; row += 4) {
+    for (int row = wave; row < kSelectRows; row += kSelectWaves) {
       const int32_t i = i0 + row;
       if (i >= a.nbq) break;
       uint8_t* out = a.map + ((int64_t)bh * a.nbq + i) * a.nbk;
@@ -152,8 +162,21 @@ __global__ __launch_bounds__(256) void psa_select_kernel(SelectArgs a) {
         return c;
       };
       if (search) {
-        int32_t c = a.first_k;
-        for (int bit = 63; bit >= 0 && c != kept; bit--) {
+        int32_t c = a.first_k, bit = 63;
+        if constexpr (R > 0) {
+          // the upper halves first: they nearly always decide, and compare at four times the rate
+          for (; bit >= 32 && c != kept; bit--) {
+            const uint32_t t = (uint32_t)(low >> 32) | (1u << (bit - 32));
+            int32_t ct = 0;
+#pragma unroll
+            for (int r = 0; r < R; r++) ct += __builtin_popcountll(__builtin_amdgcn_ballot_w64((uint32_t)(v[r] >> 32) >= t));
+            if (ct >= kept) {
+              low = (uint64_t)t << 32;
+              c = ct;
+            }
+          }
+        }
+        for (; bit >= 0 && c != kept; bit--) {
           const uint64_t t = low | (1ull << bit);
           const int32_t ct = count(t);
           if (ct >= kept) {
@@ -189,10 +212,12 @@ __global__ __launch_bounds__(256) void psa_select_kernel(SelectArgs a) {
 
 }  // namespace
 
-// Score words per lane: up to 10 in LDS, up to 20 through the slab, else none.
-static int select_regs(int32_t first_k) { return first_k <= SelectForm<10, true>::kCap ? 10 : first_k <= 64 * 20 ? 20 : 0; }
+// Score words per lane and row for these key blocks (before the text): 5 or 10 from LDS, 20 through the slab, else none.
+static int select_regs(int32_t first_k) {
+  return first_k <= 64 * 5 ? 5 : first_k <= kSelectLds ? 10 : first_k <= 64 * 20 ? 20 : 0;
+}
 
-// Workgroups of a launch: two per CU.
+// Workgroups that have a slab each: two per CU.
 constexpr int32_t kSelectGroups = 512;
 
 SelectLayout select_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk) {
@@ -202,7 +227,7 @@ SelectLayout select_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t
   l.mean_k = up((size_t)n_bh * nbq * head_dim * sizeof(double));
   l.scores = l.mean_k + up((size_t)n_kv * nbk * head_dim * sizeof(double));
   // (sized for every key block: the text may be none)
-  const size_t slab = select_regs(nbk) == 10 ? 0 : (size_t)kSelectGroups * kSelectRows * nbk * sizeof(uint64_t);
+  const size_t slab = nbk <= kSelectLds ? 0 : (size_t)kSelectGroups * kSelectRows * nbk * sizeof(uint64_t);
   l.total = l.scores + up(slab);
   return l;
 }
@@ -210,9 +235,10 @@ SelectLayout select_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t
 hipError_t launch_select(const SelectArgs& args, int32_t head_dim, hipStream_t stream) {
   SelectArgs a = args;
   a.q_blocks_all = a.n_bh * a.nbq;
-  a.slab = a.nbk;
-  const int32_t items = a.n_bh * ((a.nbq + kSelectRows - 1) / kSelectRows);
-  const int32_t grid = std::min(kSelectGroups, (items + kNumQueues - 1) / kNumQueues * kNumQueues);
+  a.slab = std::max(a.first_k, 1);
+  const int32_t items = (a.n_bh * ((a.nbq + kSelectRows - 1) / kSelectRows) + kNumQueues - 1) / kNumQueues * kNumQueues;
+  const int32_t slabs = std::min(kSelectGroups, items);
+  const int32_t bytes = kSelectRows * a.slab * (int32_t)sizeof(uint64_t);
   const dim3 means(a.q_blocks_all + (a.n_bh / a.group) * a.nbk);
   auto go = [&](auto dim) {
     constexpr int D = decltype(dim)::value;
@@ -220,9 +246,10 @@ hipError_t launch_select(const SelectArgs& args, int32_t head_dim, hipStream_t s
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     switch (select_regs(a.first_k)) {
-      case 10: hipLaunchKernelGGL((psa_select_kernel<D, 10, true>), dim3(grid), dim3(256), 0, stream, a); break;
-      case 20: hipLaunchKernelGGL((psa_select_kernel<D, 20, false>), dim3(grid), dim3(256), 0, stream, a); break;
-      default: hipLaunchKernelGGL((psa_select_kernel<D, 0, false>), dim3(grid), dim3(256), 0, stream, a);
+      case 5: hipLaunchKernelGGL((psa_select_kernel<D, 5, true>), dim3(items), dim3(64 * kSelectWaves), bytes, stream, a); break;
+      case 10: hipLaunchKernelGGL((psa_select_kernel<D, 10, true>), dim3(items), dim3(64 * kSelectWaves), bytes, stream, a); break;
+      case 20: hipLaunchKernelGGL((psa_select_kernel<D, 20, false>), dim3(slabs), dim3(64 * kSelectWaves), 0, stream, a); break;
+      default: hipLaunchKernelGGL((psa_select_kernel<D, 0, false>), dim3(slabs), dim3(64 * kSelectWaves), 0, stream, a);
     }
     return hipGetLastError();
   };
