@@ -820,7 +820,10 @@ psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, i
   a.part_o = (float*)workspace;
   a.part_ml = (float2*)((char*)workspace + l.part_ml);
   a.row_counts = (int32_t*)workspace;
-  a.row_order = (int32_t*)((char*)workspace + l.order);
+  a.row_order = (int32_t*)((char*)workspace + l.row_order);
+  a.pair_counts = (int32_t*)((char*)workspace + l.pair_counts);
+  a.pair_order = (int32_t*)((char*)workspace + l.pair_order);
+  a.paired = (int32_t*)((char*)workspace + l.paired);
   const hipError_t e = psa::launch_map_fwd(a, head_dim, stream);
   return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_attention_map_fwd launch");
 }

@@ -1732,153 +1732,6 @@ __global__ __launch_bounds__(64) void psa_rearm_kernel(int32_t* __restrict__ que
 //     few items (launch_dense).
 // ---------------------------------------------------------------------------------------------
 
-// Entry i of a pair's block stream: key block in bits 0-12, kept by the first row (bit 13) and
-// by the second row (bit 14).
-constexpr int kEntryRowShift = 13;
-constexpr int kEntryBlockMask = (1 << kEntryRowShift) - 1;
-static_assert(PSA_MAX_BLOCKS <= (1 << kEntryRowShift), "block index fits the entry");
-
-// One work item of the pair engine: this wave's row (block of BLK query rows, -1: none) of one
-// (batch, head) and nu stream entries (SPARSE: in `list`; dense: every block, kept by both rows).
-// Block i sits in buffer i & 1; after one barrier (its loads, issued a block earlier, have landed
-// and block i - 1 is no longer read) the loads of block i + 1 go out and each row that keeps block
-// i runs it: Q K^T, softmax and P V for each step of 64 keys.
-template <int D, int BLK, int SUB, bool SPARSE, bool PAD>
-__device__ __forceinline__ void process_pair(const DmaPlan<D, BLK>& plan, int grp,
-                                             const __bf16* __restrict__ qh,
-                                             const __bf16* __restrict__ kh,
-                                             const __bf16* __restrict__ vh,
-                                             __bf16* __restrict__ oh, float* __restrict__ lseh,
-                                             int n, int my_row, int nu, int first,
-                                             const uint16_t* list, float c,
-                                             uint8_t (*sk)[Tile<D, BLK>::BYTES],
-                                             uint8_t (*sv)[Tile<D, BLK>::BYTES],
-                                             const uint64_t* masks) {
-  using T = Tile<D, BLK>;
-  using H = Half<D, BLK>;
-  const int tid = threadIdx.x, lane = tid & 63, gw = (tid >> 6) & (T::kWaves - 1);
-  const int h = lane >> 5, r32 = lane & 31;
-  const int row = my_row * BLK + gw * 32 + r32;
-
-  // Entry i of the stream: list entry first + i, cyclically (SUB = 2: half i % 2 of list entry
-  // first + i / 2, kept by both groups).  Dense: block i, kept by both rows, in a word that numbers any
-  // number of blocks (its streams can be longer than a list).
-  constexpr int kRowShift = SPARSE ? kEntryRowShift : 30;
-  auto entry = [&](int i) {
-    if constexpr (SPARSE) {
-      int j = i / SUB + first;
-      const int len = nu / SUB;
-      j = j >= len ? j - len : j;
-      const int x = (int)__builtin_amdgcn_readfirstlane(list[j]);
-      return SUB == 1 ? x : (x & kEntryBlockMask) * SUB + i % SUB;
-    } else {
-      return (int)((uint32_t)i | (3u << kRowShift));
-    }
-  };
-  auto block_of = [](int x) { return SUB == 1 ? x & ((1 << kRowShift) - 1) : x; };
-  // The second half of the sequence's last block may lie past the end altogether; it is loaded
-  // from the last half that does not, and masked.
-  auto from = [&](int kb) { return SUB == 1 ? kb : min(kb, (n - 1) / BLK); };
-  auto issue_k = [&](int buf, int kb) { issue_block<D, BLK>(plan, kh, lds_address(sk[buf]), from(kb), n); };
-  auto issue_v = [&](int buf, int kb) { issue_block<D, BLK>(plan, vh, lds_address(sv[buf]), from(kb), n); };
-  int e = 0;
-  // Sparse: the first block's loads go out before the Q loads, so that the two latencies overlap
-  // at the start of the item (dense: after them; the other order measured slower there).
-  if constexpr (SPARSE) {
-    if (nu > 0) {
-      e = entry(0);
-      issue_k(0, block_of(e));
-      issue_v(0, block_of(e));
-    }
-  }
-
-  WaveState<D, BLK> st;
-  if (my_row >= 0) {
-    const bf16x8* src = (const bf16x8*)(qh + (size_t)min(row, n - 1) * D) + h;
-#pragma unroll
-    for (int cc = 0; cc < T::DC; cc++) st.q[cc] = src[2 * cc];
-#pragma unroll
-    for (int cc = 0; cc < T::DC; cc++)
-      st.q[cc] = __builtin_convertvector(__builtin_convertvector(st.q[cc], f32x8) * c, bf16x8);
-#pragma unroll
-    for (int cc = 0; cc < T::DC; cc++) asm volatile("" ::"v"(st.q[cc]));
-  }
-  st.m = -__builtin_inff();
-  st.l = 0.0f;
-  st.set_neg_max(0.0f);
-  int fresh = 1;
-#pragma unroll
-  for (int dt = 0; dt < T::DT; dt++) st.o[dt] = (f32x16){};
-
-  if constexpr (!SPARSE) {
-    if (nu > 0) {
-      e = entry(0);
-      issue_k(0, block_of(e));
-      issue_v(0, block_of(e));
-    }
-  }
-  // The validity words of a block (one word per 64 positions) are read when its loads are issued, a block
-  // ahead: read where they are needed they put a scalar load into the chain of every block.  Not with
-  // SUB = 2, whose four waves per SIMD hide that load and have no registers left.
-  uint64_t lo_next = ~0ull, hi_next = ~0ull;
-  auto read_masks = [&](int kb) {
-    if constexpr (PAD) {
-      lo_next = masks[SUB == 1 ? 2 * kb : kb];
-      if constexpr (BLK > 64) hi_next = masks[2 * kb + 1];
-    }
-  };
-  if (SUB == 1 && nu > 0) read_masks(block_of(e));
-  // Where the loop's instructions lie within the fetch lines moves the dense kernel of head dim 128 by up
-  // to 1.5 % (75600 tokens, 40 heads: 98.0 to 99.3 ms over 13 offsets); this is the best one measured.
-  if constexpr (!SPARSE && D == 128 && BLK == 128) asm volatile(".p2align 8\n\ts_nop 0\n\ts_nop 0\n\ts_nop 0");
-  for (int i = 0; i < nu; i++) {
-    const int kb = block_of(e);
-    const bool mine = my_row >= 0 && (SUB > 1 || ((e >> (kRowShift + grp)) & 1));
-    if constexpr (SUB > 1) read_masks(kb);
-    const uint64_t lo = lo_next, hi = hi_next;
-    const bool tail = PAD ? (BLK > 64 ? lo & hi : lo) != ~0ull : (kb + 1) * BLK > n;
-    wait_dma<0>();                                        // block i, issued a block ago
-    __syncthreads();                                      // ... by every wave; block i-1 read
-    // The next block's K goes out right after the barrier and its V after this block's first
-    // Q K^T half: a wave stalls while it issues, and a single burst of all its loads after the
-    // barrier, where every wave issues at once, keeps the MFMA pipes idle for longer (measured:
-    // sparse 0.5-1.3 % and dense 0.4-3 % faster on two boxes, same bits).
-    const bool more = i + 1 < nu;
-    int kbn = 0;
-    if (more) {
-      e = entry(i + 1);
-      kbn = block_of(e);
-      if constexpr (SUB == 1) read_masks(kbn);
-      issue_k((i + 1) & 1, kbn);
-    }
-    if (mine) {
-      const uint8_t* skb = sk[i & 1];
-      const uint8_t* svb = sv[i & 1];
-      f32x16 s[H::KT];
-      qk_half<D, BLK>(st, s, skb, 0, lane);
-      if (more) issue_v((i + 1) & 1, kbn);
-      softmax_pv_half<D, BLK, PAD>(st, s, svb, kb, 0, n, tail, lo, hi, lane, fresh);
-      if constexpr (BLK > H::HK) {
-        qk_half<D, BLK>(st, s, skb, H::HK, lane);
-        softmax_pv_half<D, BLK, PAD>(st, s, svb, kb, H::HK, n, tail, lo, hi, lane, fresh);
-      }
-    } else if (more) {
-      issue_v((i + 1) & 1, kbn);
-    }
-  }
-  if constexpr (SPARSE) {
-    // The buffer of block nu - 2 (every wave passed the barrier of block nu - 1) stages the
-    // output: 8 KB per wave, K half for group 0, V half for group 1.
-    if (my_row >= 0) {
-      static_assert(T::kWaves * 32 * 2 * D <= T::BYTES, "a wave's rows fit its share of a free buffer");
-      const uint32_t stage = lds_address(grp == 0 ? sk[nu & 1] : sv[nu & 1]) + gw * (32 * 2 * D);
-      store_rows_staged<D, BLK>(st, oh, lseh, my_row * BLK + gw * 32, n, lane, stage);
-    }
-  } else {
-    if (my_row >= 0) store_rows<D, BLK>(st, oh, lseh, row, n, lane);
-  }
-}
-
 // SPARSE: persistent, workgroups popping pair items (SUB parts each) from the plan's queues.  Dense:
 // the pairs (2 p, 2 p + 1) of the flattened (batch*head, pair) list, either popped from armed queues
 // by a persistent grid (queues given) or one per workgroup, consecutive workgroups of one XCD taking
@@ -2018,7 +1871,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(PairSha
     }
     const size_t off = (size_t)bh * n * D;
     process_pair<D, BLK, SUB, SPARSE, PAD>(plan, grp, q + off, k + off, v + off, o + off,
-                                      lse ? lse + (size_t)bh * n : nullptr, n, my_row, nu, first, list,
+                                      lse ? lse + (size_t)bh * n : nullptr, n, n, my_row, nu, first, list,
                                       c, sk, sv, masks);
   }
 }

@@ -292,6 +292,8 @@ struct MapArgs {
   float *neg_lse2, *neg_delta;        // backward: [n_bh][nbq][block]
   __bf16* q_scaled;                   // backward: bf16(scale log2(e) q), like q
   int32_t *row_counts, *row_order;    // list lengths of the (head, query block) items and their order
+  int32_t *pair_counts, *pair_order;  // forward, block 64: those of pairs of query blocks, and
+  int32_t* paired;                    // whether pairs run (null: they do not)
   int32_t *col_counts, *col_order;    // backward: those of the (key head, key block) items
   int32_t n_bh, n_heads, group;       // group: query heads per key head
   int32_t n_q, n_k, nbq, nbk, block, parts;
@@ -299,7 +301,8 @@ struct MapArgs {
 };
 struct MapLayout {
   int32_t parts;
-  size_t part_ml, order, total;       // part_o first, or, in one part, the items' list lengths
+  size_t part_ml, total;              // in parts (part_o first)
+  size_t row_order, pair_counts, pair_order, paired;  // in one part (row_counts first)
 };
 MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);

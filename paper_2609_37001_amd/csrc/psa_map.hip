@@ -71,24 +71,55 @@ __device__ __forceinline__ int32_t item_of(int32_t blk, int32_t items) {
   return blk >= part * kNumQueues ? blk : blk % kNumQueues * part + blk / kNumQueues;
 }
 
+// Whether maps of 64 run on pairs of query blocks: `either` counts the key blocks that one block of a pair or both keep,
+// `single` those that each keeps, over all pairs.  A wave waits while its neighbour's block alone is worked on, so
+// pairs pay where neighbours share enough; at head dim 64, whose four waves per SIMD cover such waits, in long lists
+// always.  Microseconds in pairs and one by one at either / single 0.88, 0.71 and 0.50:
+//   head dim 64   12 heads x 32760, density 0.25 (3072 pairs)  1102, 963, 861 and 1259, 1191, 1190
+//                 8 x 8000, 0.2 (504 pairs)                    81, 71, 58     and 69, 70, 70
+//   head dim 128  12 x 32760, 0.25                             2039, 1779, 1540 and 1840, 1820, 1822
+//                 8 x 8000, 0.2                                105, 88, 78    and 94, 94, 92
+constexpr int32_t kManyPairs = 2048;        // twice the workgroups that run at once
+__device__ __forceinline__ bool pairs_pay(unsigned long long either, unsigned long long single, int32_t pairs, int32_t head_dim) {
+  return head_dim == 64 ? pairs >= kManyPairs || either * 100 <= single * 73 : either * 10 <= single * 7;
+}
+
 // ---------------------------------------------------------------------------------------------
 // Order of the items: those with long lists first.  Where the items outnumber the workgroups that run at once, a
 // long one that starts late is waited for alone (a row of text, a key block that everybody keeps).  Items whose
 // lists are about as long stay in their order, for the XCDs' sake.
 // ---------------------------------------------------------------------------------------------
 
-// Kept key blocks of every (head, query block), a wave each.
+// The two query blocks of pair p of a map's head: 2 p and 2 p + 1 (-1 behind an odd number of them).
+__device__ __forceinline__ int2 pair_of(int32_t p, int32_t nbq) { return make_int2(2 * p, 2 * p + 1 < nbq ? 2 * p + 1 : -1); }
+
+// Kept key blocks of every (head, query block), and, if asked, those that either block of a pair keeps; a wave per pair.
 __global__ __launch_bounds__(256) void psa_mapped_row_count_kernel(MapArgs a) {
-  const int32_t item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (item >= a.n_bh * a.nbq) return;
-  const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
-  const uint8_t* row = a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk;
-  int32_t c = 0;
-#pragma unroll 8
-  for (int32_t j = lane; j < a.nbk; j += 64) c += row[j] != 0;
+  const int32_t item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, np = pairs_per_head(a.nbq);
+  if (item >= a.n_bh * np) return;
+  const int32_t bh = item / np, b = bh / a.n_heads, hd = bh - b * a.n_heads;
+  const int2 pr = pair_of(item - bh * np, a.nbq);
+  const uint8_t* first = a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + pr.x) * a.nbk;
+  const uint8_t* second = pr.y < 0 ? first : first + a.nbk;
+  int32_t c0 = 0, c1 = 0, both = 0;
+#pragma unroll 4
+  for (int32_t j = lane; j < a.nbk; j += 64) {
+    const bool x = first[j] != 0, y = second[j] != 0;
+    c0 += x;
+    c1 += y;
+    both += x || y;
+  }
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) c += __shfl_xor(c, off);
-  if (lane == 0) a.row_counts[item] = c;
+  for (int off = 32; off > 0; off >>= 1) {
+    c0 += __shfl_xor(c0, off);
+    c1 += __shfl_xor(c1, off);
+    both += __shfl_xor(both, off);
+  }
+  if (lane == 0) {
+    a.row_counts[bh * a.nbq + pr.x] = c0;
+    if (pr.y >= 0) a.row_counts[bh * a.nbq + pr.y] = c1;
+    if (a.pair_counts) a.pair_counts[item] = both;
+  }
 }
 
 // Kept (query head, query block) pairs of every (key head, key block); 64 key blocks per workgroup.
@@ -107,27 +138,43 @@ __global__ __launch_bounds__(256) void psa_mapped_col_count_kernel(MapArgs a) {
   if (wave == 0 && kb < a.nbk) a.col_counts[bk * a.nbk + kb] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
 }
 
+// Sum of a list over the workgroup, in every thread.
+__device__ __forceinline__ unsigned long long list_sum(const int32_t* counts, int32_t n, unsigned long long* total) {
+  __syncthreads();
+  if (threadIdx.x == 0) *total = 0;
+  __syncthreads();
+  unsigned long long mine = 0;
+  for (int32_t i = threadIdx.x; i < n; i += blockDim.x) mine += counts[i];
+  atomicAdd(total, mine);
+  __syncthreads();
+  return *total;
+}
+
 // order[workgroup] = item: eight classes of list lengths around the mean, longest first, each in the items' order and
-// spread over the XCDs.  One workgroup per list of items (rows, columns); each thread takes a run of them.
+// spread over the XCDs.  One workgroup per list of items; each thread takes a run of them.  Pairs' lists come second:
+// their workgroup also says whether they pay (pairs_pay).
 constexpr int kOrderThreads = 1024, kOrderClasses = 8;
-__global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(const int32_t* __restrict__ counts0, int32_t* __restrict__ order0,
-                                                                         int32_t n0, const int32_t* __restrict__ counts1,
-                                                                         int32_t* __restrict__ order1, int32_t n1) {
+struct OrderList {
+  const int32_t* counts;
+  int32_t* order;
+  int32_t n;
+};
+__global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(OrderList l0, OrderList l1, int32_t* __restrict__ paired,
+                                                                         int32_t head_dim) {
   __shared__ int32_t at[kOrderClasses * kOrderThreads];
   __shared__ int32_t waves[kOrderThreads / 64];
   __shared__ unsigned long long total;
-  const int32_t* counts = blockIdx.x ? counts1 : counts0;
-  int32_t* order = blockIdx.x ? order1 : order0;
-  const int32_t n = blockIdx.x ? n1 : n0;
+  const int32_t* counts = blockIdx.x ? l1.counts : l0.counts;
+  int32_t* order = blockIdx.x ? l1.order : l0.order;
+  const int32_t n = blockIdx.x ? l1.n : l0.n;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int32_t each = (n + kOrderThreads - 1) / kOrderThreads, i0 = min(n, tid * each), i1 = min(n, i0 + each);
-  if (tid == 0) total = 0;
-  __syncthreads();
-  unsigned long long mine = 0;
-  for (int32_t i = i0; i < i1; i++) mine += counts[i];
-  atomicAdd(&total, mine);
-  __syncthreads();
-  const float mean = (float)total / (float)n;
+  const unsigned long long work = list_sum(counts, n, &total);
+  if (paired && blockIdx.x == 1) {
+    const unsigned long long single = list_sum(l0.counts, l0.n, &total);
+    if (tid == 0) *paired = pairs_pay(work, single, n, head_dim) ? 1 : 0;
+  }
+  const float mean = (float)work / (float)n;
   auto cls = [&](int32_t c) {
     const float x = (float)c;
     return x >= 4.0f * mean ? 0 : x >= 2.83f * mean ? 1 : x >= 2.0f * mean ? 2 : x >= 1.5f * mean ? 3 :
@@ -322,6 +369,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ float2 stat[W][32];              // (m, l) of every wave's rows
   extern __shared__ uint16_t list[];          // nbk entries
 
+  if (BLK == 64 && !SPLIT && a.paired && *a.paired) return;   // (psa_mapped_pairs_kernel runs)
   const int32_t whole = a.row_order ? a.row_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
   const int32_t item = SPLIT ? whole / a.parts : whole, part = SPLIT ? whole - item * a.parts : 0;
   const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
@@ -437,6 +485,53 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
     else if (a.lse)
       a.lse[place] = lsum > 0.0f ? (top + __builtin_log2f(lsum)) * 0.69314718055994530942f : -__builtin_inff();
   }
+}
+
+// Maps of 64 on pairs: a workgroup of the pair engine (psa_tile.h) takes two neighbouring query blocks, which share one
+// stream of the key blocks that either keeps; a wave works through whole blocks of 64 keys where the kernel above
+// gives it 32.  Neighbours that keep much the same blocks gain by it, see pairs_pay.
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) void psa_mapped_pairs_kernel(MapArgs a) {
+  constexpr int BLK = 64;
+  using T = Tile<D, BLK>;
+  constexpr int W = 2 * T::kWaves;
+  __shared__ __attribute__((aligned(1024))) uint8_t sk[2][T::BYTES];
+  __shared__ __attribute__((aligned(1024))) uint8_t sv[2][T::BYTES];
+  __shared__ int32_t found[W];
+  extern __shared__ uint16_t list[];          // nbk entries
+  if (*a.paired == 0) return;
+  const int32_t np = pairs_per_head(a.nbq), item = a.pair_order[blockIdx.x];
+  const int32_t bh = item / np, b = bh / a.n_heads, hd = bh - b * a.n_heads;
+  const int2 pr = pair_of(item - bh * np, a.nbq);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
+  const uint8_t* first = a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + pr.x) * a.nbk;
+  int32_t nu = 0;
+  for (int32_t base = 0; base < a.nbk; base += W * 64) {
+    const int32_t kb = base + tid;
+    const bool x = kb < a.nbk && first[kb] != 0, y = kb < a.nbk && pr.y >= 0 && first[(int64_t)a.nbk + kb] != 0;
+    const uint64_t mask = __builtin_amdgcn_ballot_w64(x || y);
+    if (lane == 0) found[wave] = __builtin_popcountll(mask);
+    __syncthreads();
+    int32_t pos = nu;
+#pragma unroll
+    for (int w = 0; w < W; w++) {
+      pos += w < wave ? found[w] : 0;
+      nu += found[w];
+    }
+    if (x || y)
+      list[pos + __builtin_popcountll(mask & ((1ull << lane) - 1))] =
+          (uint16_t)(kb | (x ? 1 << kEntryRowShift : 0) | (y ? 2 << kEntryRowShift : 0));
+    __syncthreads();
+  }
+  nu = __builtin_amdgcn_readfirstlane(nu);
+  DmaPlan<D, BLK> plan;
+  plan.init(__builtin_amdgcn_readfirstlane(wave), lane);
+  const int64_t kv_off = b * a.kv_stride_b + (hd / a.group) * a.kv_stride_h, off = (int64_t)bh * a.n_q;
+  process_pair<D, BLK, 1, true, false>(plan, grp, a.q + off * D, a.k + kv_off, a.v + kv_off, a.o + off * D,
+                                       a.lse ? a.lse + off : nullptr, a.n_q, a.n_k,
+                                       __builtin_amdgcn_readfirstlane(grp == 0 ? pr.x : pr.y), nu, 0, list, a.c, sk, sv,
+                                       nullptr);
 }
 
 // Adds the parts of every query row: o = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p.  D / 4 lanes a row.
@@ -745,8 +840,12 @@ MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, i
     l.part_ml = up256(rows * head_dim * sizeof(float));
     l.total = l.part_ml + up256(rows * sizeof(float2));
   } else if (ordered(items, block)) {
-    l.order = up256(items * sizeof(int32_t));
-    l.total = 2 * l.order;
+    const size_t pairs = up256((size_t)n_bh * pairs_per_head(nbq) * sizeof(int32_t));
+    l.row_order = up256(items * sizeof(int32_t));
+    l.pair_counts = 2 * l.row_order;
+    l.pair_order = l.pair_counts + pairs;
+    l.paired = l.pair_order + pairs;
+    l.total = l.paired + 256;
   }
   return l;
 }
@@ -767,36 +866,43 @@ MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_
 }
 
 // The orders of the rows and columns that outnumber the workgroups; clears the pointers of the others.
-static hipError_t launch_orders(MapArgs& a, bool cols, hipStream_t stream) {
+static hipError_t launch_orders(MapArgs& a, int32_t head_dim, bool cols, hipStream_t stream) {
   const int32_t n0 = a.n_bh * a.nbq, n1 = a.n_bh / a.group * a.nbk;
   const bool by_row = ordered(n0, a.block), by_col = cols && ordered(n1, a.block);
   if (!by_row) a.row_order = nullptr;
   if (!by_col) a.col_order = nullptr;
+  if (!by_row || cols || a.block != 64) a.paired = a.pair_counts = nullptr;
   if (!by_row && !by_col) return hipSuccess;
-  if (by_row) hipLaunchKernelGGL(psa_mapped_row_count_kernel, dim3((n0 + 3) / 4), dim3(256), 0, stream, a);
+  const int32_t pairs = a.n_bh * pairs_per_head(a.nbq);
+  if (by_row) hipLaunchKernelGGL(psa_mapped_row_count_kernel, dim3((pairs + 3) / 4), dim3(256), 0, stream, a);
   if (by_col)
     hipLaunchKernelGGL(psa_mapped_col_count_kernel, dim3((a.nbk + 63) / 64 * (a.n_bh / a.group)), dim3(256), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int32_t *c0 = by_row ? a.row_counts : a.col_counts, *c1 = a.col_counts;
-  int32_t *o0 = by_row ? a.row_order : a.col_order, *o1 = a.col_order;
-  hipLaunchKernelGGL(psa_mapped_order_kernel, dim3(by_row + by_col), dim3(kOrderThreads), 0, stream, c0, o0, by_row ? n0 : n1,
-                     c1, o1, n1);
+  const OrderList rows = {a.row_counts, a.row_order, n0}, col = {a.col_counts, a.col_order, n1};
+  const OrderList pair = {a.pair_counts, a.pair_order, pairs};
+  hipLaunchKernelGGL(psa_mapped_order_kernel, dim3(by_row + (by_col || a.paired)), dim3(kOrderThreads), 0, stream,
+                     by_row ? rows : col, a.paired ? pair : col, a.paired, head_dim);
   return hipGetLastError();
 }
 
 hipError_t launch_map_fwd(const MapArgs& args, int32_t head_dim, hipStream_t stream) {
   MapArgs a = args;
-  hipError_t e = a.parts == 1 ? launch_orders(a, false, stream) : hipSuccess;
+  if (a.parts > 1) a.row_order = a.paired = nullptr;
+  const hipError_t e = a.parts == 1 ? launch_orders(a, head_dim, false, stream) : hipSuccess;
   if (e != hipSuccess) return e;
   return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
     constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
     const dim3 grid(a.n_bh * a.nbq * a.parts);
     if (a.parts == 1) {
+      if constexpr (B == 64) {
+        if (a.paired)
+          hipLaunchKernelGGL((psa_mapped_pairs_kernel<D>), dim3(a.n_bh * pairs_per_head(a.nbq)), dim3(256),
+                             list_bytes(a.nbk), stream, a);
+      }
       hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, false>), grid, dim3(4 * B), list_bytes(a.nbk), stream, a);
       return hipGetLastError();
     }
-    a.row_order = nullptr;
     hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, true>), grid, dim3(4 * B), list_bytes(a.nbk), stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -808,7 +914,7 @@ hipError_t launch_map_fwd(const MapArgs& args, int32_t head_dim, hipStream_t str
 
 hipError_t launch_map_bwd(const MapArgs& args, int32_t head_dim, hipStream_t stream) {
   MapArgs a = args;
-  hipError_t e = launch_orders(a, true, stream);
+  hipError_t e = launch_orders(a, head_dim, true, stream);
   if (e != hipSuccess) return e;
   return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
     constexpr int D = decltype(dim)::value, B = decltype(blk)::value;

@@ -157,6 +157,21 @@ def test_one_workgroup_per_query_block(d, block):
 
 
 @pytest.mark.parametrize("d,block", SHAPES)
+@pytest.mark.parametrize("h,hk,alike", [(140, 70, 0.0), (140, 140, 0.9), (840, 420, 0.0)])
+def test_many_query_blocks(d, block, h, hk, alike):
+    """More query and key blocks than run at once, in the order of their lists; neighbouring rows that keep other
+    or much the same key blocks, an odd number of rows, long and empty ones."""
+    nq, nk = 5, 7
+    m = random_map(31, 1, h, nq, nk, 0.5)
+    rng = np.random.default_rng(32)
+    same = rng.random((1, h, nq, nk)) < alike
+    m[:, :, 1::2] = np.where(same[:, :, 1::2], m[:, :, 0:nq - 1:2], m[:, :, 1::2])
+    m[:, ::3, 2] = 1
+    m[:, 1::7] = 0
+    check(1, h, hk, 4 * block + 17, 6 * block + 33, block, d, m=m, heads=[0, 1, 2, h - 1])
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
 @pytest.mark.parametrize("h,hk", [(4, 2), (6, 1), (8, 8)])
 def test_shared_key_heads(d, block, h, hk):
     check(2, h, hk, 300, 450, block, d)
