@@ -446,6 +446,18 @@ def l2_distance(o, ref, sq_err=None, sq_ref=None, workspace=None, stream=None):
 # Norms and rotary positions of queries and keys (include/psa.h, fourth part).
 # ---------------------------------------------------------------------------------------------
 
+def _on_device(device, stream):
+    """Contexts of a call: the tensors' device and the stream given.  Nothing to enter where both are the current
+    ones (two contexts cost as much host time as the launch of a small call)."""
+    torch = _torch()
+    if stream is None and device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    stack = contextlib.ExitStack()
+    stack.enter_context(torch.cuda.device(device))
+    stack.enter_context(_on(stream))
+    return stack
+
+
 def _rows(x, name, dtype, tokens, like=None):
     """psa_rows_t of x, [batch, heads, N, head_dim] of any strides with the channels side by side."""
     torch = _torch()
@@ -453,31 +465,33 @@ def _rows(x, name, dtype, tokens, like=None):
         raise TypeError("%s must be bfloat16 or float32, queries and keys alike" % name)
     if not x.is_cuda:
         raise ValueError("%s must be a GPU tensor" % name)
-    if x.dim() != 4 or x.stride(3) != 1:
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 4 or stride[3] != 1:
         raise ValueError("%s must be [batch, heads, N, head_dim] with contiguous channels" % name)
-    if x.shape[2] != tokens:
-        raise ValueError("%s has %d tokens, the grid %d" % (name, x.shape[2], tokens))
-    if like is not None and (x.device != like.device or x.shape[0] != like.shape[0] or x.shape[3] != like.shape[3]):
+    if shape[2] != tokens:
+        raise ValueError("%s has %d tokens, the grid %d" % (name, shape[2], tokens))
+    if like is not None and (x.device != like.device or shape[0] != like.shape[0] or shape[3] != like.shape[3]):
         raise ValueError("%s must share the queries' batch, head_dim and device" % name)
-    b, h, n = (s if size > 1 else 0 for s, size in zip(x.stride()[:3], x.shape))
-    return _lib.Rows(x.data_ptr(), b, h, n, x.shape[1])
+    return _lib.Rows(x.data_ptr(), stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0,
+                     stride[2] if shape[2] > 1 else 0, shape[1])
 
 
 def _rope(grid, axes, theta, origin, pairing):
     if pairing not in ("adjacent", "halves"):
         raise ValueError('pairing is "adjacent" or "halves"')
-    g, a, o = _grid(grid), tuple(int(x) for x in axes), tuple(int(x) for x in origin)
+    a, o = tuple(map(int, axes)), tuple(map(int, origin))
     if len(a) != 3 or len(o) != 3:
         raise ValueError("axes and origin have three entries (time, height, width)")
-    return _lib.Rope(g, *o, *a, _lib.PAIRS_HALVES if pairing == "halves" else _lib.PAIRS_ADJACENT, float(theta))
+    return _lib.Rope(_grid(grid), *o, *a, _lib.PAIRS_HALVES if pairing == "halves" else _lib.PAIRS_ADJACENT, theta)
 
 
 def _norm_weight(w, x, name):
+    if w is None:
+        return
     torch = _torch()
-    if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (x.shape[3],) or not w.is_contiguous()
-                          or w.device != x.device):
+    if (w.dtype != torch.float32 or tuple(w.shape) != (x.shape[3],) or not w.is_contiguous()
+            or w.device != x.device):
         raise ValueError("%s must be a contiguous float32 tensor [head_dim] on the queries' device" % name)
-    return w
 
 
 def _attention_layout(x, like, name):
@@ -485,7 +499,6 @@ def _attention_layout(x, like, name):
     torch = _torch()
     if x.dtype != torch.bfloat16 or x.shape != like.shape or not x.is_contiguous() or x.device != like.device:
         raise ValueError("%s must be a contiguous bfloat16 tensor %s on the queries' device" % (name, tuple(like.shape)))
-    return x
 
 
 def _type_of(x):
@@ -516,11 +529,16 @@ def qk_norm_rope(q, k, grid, axes, q_weight=None, k_weight=None, norm=True, eps=
     rope = _rope(grid, axes, theta, origin, pairing)
     _norm_weight(q_weight, q, "q_weight")
     _norm_weight(k_weight, q, "k_weight")
-    with torch.cuda.device(q.device), _on(stream):
-        yq = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if q_out is None else _attention_layout(q_out, q, "q_out")
-        yk = None
-        if k is not None:
-            yk = torch.empty(k.shape, dtype=torch.bfloat16, device=q.device) if k_out is None else _attention_layout(k_out, k, "k_out")
+    with _on_device(q.device, stream):
+        yq, yk = q_out, k_out if k is not None else None
+        if yq is None:
+            yq = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        else:
+            _attention_layout(yq, q, "q_out")
+        if yk is not None:
+            _attention_layout(yk, k, "k_out")
+        elif k is not None:
+            yk = torch.empty(k.shape, dtype=torch.bfloat16, device=q.device)
         _lib.check(_lib.lib().psa_qk_norm_rope_fwd(
             rq, rk, _ptr(yq), _ptr(yk), _type_of(q), q.shape[0], q.shape[3], rope, 1 if norm else 0, _ptr(q_weight),
             _ptr(k_weight), float(eps), _stream(None, q.device)))
@@ -554,7 +572,7 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, grid, axes, q_weight=None, k_weight=N
     _attention_layout(dq_out, q, "dq_out")
     if k is not None:
         _attention_layout(dk_out, k, "dk_out")
-    with torch.cuda.device(q.device), _on(stream):
+    with _on_device(q.device, stream):
         grads, rows = [], []
         for given, x, name in ((dq, q, "dq"), (dk, k, "dk")):
             if x is None:
@@ -656,7 +674,7 @@ def select_blocks(q, k, block, keep, q_text=0, k_text=0, blockmap=None, workspac
     b, h, n_q, d = q.shape
     n_k = k.shape[2]
     shape = (b, h, _blocks(n_q, block), _blocks(n_k, block))
-    with torch.cuda.device(q.device), _on(stream):
+    with _on_device(q.device, stream):
         m = torch.empty(shape, dtype=torch.uint8, device=q.device) if blockmap is None else blockmap
         if tuple(m.shape) != shape or m.dtype != torch.uint8 or not m.is_contiguous() or m.device != q.device:
             raise ValueError("blockmap must be a contiguous uint8 tensor %s on the queries' device" % (shape,))
@@ -683,7 +701,7 @@ def attention_map_fwd(q, k, v, blockmap, block, scale=None, out=None, return_lse
     n_k = k.shape[2]
     bm, bm_stride = _map_of(blockmap, q, n_k, block)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
-    with torch.cuda.device(q.device), _on(stream):
+    with _on_device(q.device, stream):
         o = torch.empty_like(q) if out is None else out
         _check_q(o, "out", q)
         lse = torch.empty((b, h, n_q), dtype=torch.float32, device=q.device) if return_lse else None
@@ -710,7 +728,7 @@ def attention_map_bwd(do, q, k, v, o, lse, blockmap, block, scale=None, dq=None,
         raise ValueError("lse must be a contiguous float32 tensor [batch, heads, N_q] on the queries' device")
     bm, bm_stride = _map_of(blockmap, q, n_k, block)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
-    with torch.cuda.device(q.device), _on(stream):
+    with _on_device(q.device, stream):
         dq = torch.empty_like(q) if dq is None else dq
         dk = torch.empty(k.shape, dtype=k.dtype, device=q.device) if dk is None else dk
         dv = torch.empty(k.shape, dtype=k.dtype, device=q.device) if dv is None else dv

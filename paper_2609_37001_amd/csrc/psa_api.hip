@@ -8,6 +8,7 @@
 #include <cmath>
 
 #include "psa_launch.h"
+#include "psa_map.h"
 
 namespace {
 
@@ -322,8 +323,10 @@ psa_status_t check_rope(int32_t type, int32_t batch, int32_t n_tensors, int32_t 
   int pair = 0;
   for (int i = 0; i < 3; i++) {
     a->origin[i] = origin[i];
-    for (int j = 0; j < axes[i] / 2; j++)
-      a->turns[pair++] = std::pow(rope->theta, -2.0 * j / axes[i]) * 0.15915494309189533577;    // 1 / (2 pi)
+    // theta^(-2 j / d_a) by products of its first step, each right to 2^-53: 2^-47 after the 63 of a whole head.
+    const double step = axes[i] > 0 ? std::pow(rope->theta, -2.0 / axes[i]) : 0.0;
+    double turns = 0.15915494309189533577;                                                        // 1 / (2 pi)
+    for (int j = 0; j < axes[i] / 2; j++, turns *= step) a->turns[pair++] = turns;
     if (i < 2) a->end[i] = pair;
   }
   return PSA_OK;

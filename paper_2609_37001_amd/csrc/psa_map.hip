@@ -23,6 +23,7 @@
 #include <algorithm>
 
 #include "psa_launch.h"
+#include "psa_map.h"
 #include "psa_tile.h"
 
 namespace psa {

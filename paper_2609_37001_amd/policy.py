@@ -4,10 +4,12 @@ are exempt from sparsification, since the early steps lay out the coarse structu
 LayerAttention is the per-layer runtime piece: it plans the layer's stripes once (the plan
 depends only on the sizes and the stripes, which stay fixed over the steps) and, at each step,
 runs the dense kernel during the exempt steps and the planned sparse kernel afterwards.
+SelectedAttention is the same for a layer whose kept blocks follow from its data: at each step after the
+exempt ones it keeps, for every query block, the key blocks of the highest mean score.
 """
 import math
 
-from . import dense_fwd, plan, run
+from . import _grid_tuple, attention_map_fwd, dense_fwd, plan, run, select_blocks
 
 
 class TimestepPolicy:
@@ -50,3 +52,21 @@ class LayerAttention:
             return dense_fwd(q, k, v, self.block, self.scale, out=out, stream=stream)
         return run(q, k, v, self.grid, self.block, self._planned(q.device, stream), self.scale,
                    out=out, stream=stream)
+
+
+class SelectedAttention:
+    """One attention layer under a timestep policy: q, k, v bf16 [batch, heads, N, d].  After the exempt steps
+    every query block keeps `keep` key blocks (and the text's, which grid ends with) by select_blocks."""
+
+    def __init__(self, keep, grid, block, policy, scale=None):
+        self.keep, self.grid, self.block, self.scale = int(keep), _grid_tuple(grid), int(block), scale
+        self.policy = policy
+
+    def __call__(self, q, k, v, step, out=None, stream=None):
+        f, h, w, text = self.grid
+        if q.shape[2] != f * h * w + text:
+            raise ValueError("tensors hold %d tokens, the grid %s has %d" % (q.shape[2], self.grid, f * h * w + text))
+        if self.policy.is_dense(step):
+            return dense_fwd(q, k, v, self.block, self.scale, out=out, stream=stream)
+        blockmap, _ = select_blocks(q, k, self.block, self.keep, q_text=text, k_text=text, stream=stream)
+        return attention_map_fwd(q, k, v, blockmap, self.block, self.scale, out=out, stream=stream)

@@ -355,6 +355,30 @@ def test_refusals():
             workspace=torch.empty(256, dtype=torch.uint8, device="cuda:0"))
 
 
+@pytest.mark.parametrize("block", [64, 128])
+def test_layer_under_a_timestep_policy(block):
+    """Dense steps are the dense attention; later steps the attention over the selected blocks; all blocks selected
+    are the dense attention up to the rounding of another order of its sums."""
+    from paper_2609_37001_amd.policy import SelectedAttention, TimestepPolicy
+    torch = gu.torch()
+    grid = (3, 10, 14, 33)
+    n = 3 * 10 * 14 + 33
+    q, k, v = (torch.randn(1, 3, n, 64, device="cuda:0").bfloat16() for _ in range(3))
+    layer = SelectedAttention(2, grid, block, TimestepPolicy(5, 0.2))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    dense, got = layer(q, k, v, 0), [layer(q, k, v, s) for s in (1, 4)] + [layer(q, k, v, 2, stream=side)]
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(dense, psa.dense_fwd(q, k, v, block))
+    m, _ = psa.select_blocks(q, k, block, 2, q_text=33, k_text=33)
+    ref = psa.attention_map_fwd(q, k, v, m, block)
+    assert all(torch.equal(x, ref) for x in got) and not torch.equal(ref, dense)
+    whole = SelectedAttention(99, grid, block, TimestepPolicy(5, 0.2))(q, k, v, 1)
+    assert (whole.float() - dense.float()).norm() <= gu.REL_L2_TOL * dense.float().norm()
+    with pytest.raises(ValueError):
+        layer(q[:, :, 1:].contiguous(), k, v, 1)
+
+
 def test_together_on_a_side_stream_and_in_a_graph():
     """A layer as it is used: norm and rotation, selection, attention over the map, and all the gradients back to
     the projections; eager, on another stream, and captured and replayed on new inputs."""
