@@ -458,6 +458,11 @@ def _on_device(device, stream):
     return stack
 
 
+def _like(x, dtype):
+    """An uninitialised contiguous tensor of the shape of x."""
+    return _torch().empty_like(x, dtype=dtype, memory_format=_torch().contiguous_format)
+
+
 def _rows(x, name, dtype, tokens, like=None):
     """psa_rows_t of x, [batch, heads, N, head_dim] of any strides with the channels side by side."""
     torch = _torch()
@@ -532,16 +537,16 @@ def qk_norm_rope(q, k, grid, axes, q_weight=None, k_weight=None, norm=True, eps=
     with _on_device(q.device, stream):
         yq, yk = q_out, k_out if k is not None else None
         if yq is None:
-            yq = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+            yq = _like(q, torch.bfloat16)
         else:
             _attention_layout(yq, q, "q_out")
         if yk is not None:
             _attention_layout(yk, k, "k_out")
         elif k is not None:
-            yk = torch.empty(k.shape, dtype=torch.bfloat16, device=q.device)
+            yk = _like(k, torch.bfloat16)
         _lib.check(_lib.lib().psa_qk_norm_rope_fwd(
             rq, rk, _ptr(yq), _ptr(yk), _type_of(q), q.shape[0], q.shape[3], rope, 1 if norm else 0, _ptr(q_weight),
-            _ptr(k_weight), float(eps), _stream(None, q.device)))
+            _ptr(k_weight), float(eps), _stream(None, q.device.index)))
     return yq, yk
 
 
@@ -549,7 +554,7 @@ def _empty_rows(x):
     """Uninitialised rows in the order of x (a dense tensor where x is a slice or repeats rows)."""
     torch = _torch()
     if any(s == 0 and size > 1 for s, size in zip(x.stride(), x.shape)):
-        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        return _like(x, x.dtype)
     return torch.empty_like(x)
 
 
@@ -592,7 +597,7 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, grid, axes, q_weight=None, k_weight=N
         _lib.check(_lib.lib().psa_qk_norm_rope_bwd(
             _ptr(dq_out), _ptr(dk_out) if k is not None else None, rq, rk, rows[0], rows[1], _ptr(dw[0]), _ptr(dw[1]),
             _type_of(q), q.shape[0], q.shape[3], rope, 1 if norm else 0, _ptr(q_weight), _ptr(k_weight), float(eps),
-            ws, ws_bytes, _stream(None, q.device)))
+            ws, ws_bytes, _stream(None, q.device.index)))
     return grads[0], grads[1], dw[0], dw[1]
 
 
@@ -682,7 +687,7 @@ def select_blocks(q, k, block, keep, q_text=0, k_text=0, blockmap=None, workspac
         L = _lib.lib()
         ws, nbytes, _keep = _workspace(workspace, int(L.psa_select_workspace_size(b, h, k.shape[1], d, n_q, n_k, int(block))), q.device)
         _lib.check(L.psa_select_blocks(_ptr(q), kv, b, h, d, n_q, n_k, int(block), int(keep), int(q_text), int(k_text),
-                                       _ptr(m), _ptr(kept), ws, nbytes, _stream(None, q.device)))
+                                       _ptr(m), _ptr(kept), ws, nbytes, _stream(None, q.device.index)))
     return m, kept
 
 
@@ -708,7 +713,7 @@ def attention_map_fwd(q, k, v, blockmap, block, scale=None, out=None, return_lse
         L = _lib.lib()
         ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_workspace_size(b, h, d, n_q, n_k, int(block))), q.device)
         _lib.check(L.psa_attention_map_fwd(_ptr(q), kv, _ptr(o), b, h, d, n_q, n_k, int(block), bm, bm_stride, scale,
-                                           _ptr(lse), ws, nbytes, _stream(None, q.device)))
+                                           _ptr(lse), ws, nbytes, _stream(None, q.device.index)))
     return (o, lse) if return_lse else o
 
 
@@ -730,8 +735,8 @@ def attention_map_bwd(do, q, k, v, o, lse, blockmap, block, scale=None, dq=None,
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     with _on_device(q.device, stream):
         dq = torch.empty_like(q) if dq is None else dq
-        dk = torch.empty(k.shape, dtype=k.dtype, device=q.device) if dk is None else dk
-        dv = torch.empty(k.shape, dtype=k.dtype, device=q.device) if dv is None else dv
+        dk = _like(k, k.dtype) if dk is None else dk
+        dv = _like(k, k.dtype) if dv is None else dv
         _check_q(dq, "dq", q)
         _check_q(dk, "dk", k)
         _check_q(dv, "dv", k)
@@ -739,5 +744,5 @@ def attention_map_bwd(do, q, k, v, o, lse, blockmap, block, scale=None, dq=None,
         ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_bwd_workspace_size(b, h, k.shape[1], d, n_q, n_k, int(block))), q.device)
         _lib.check(L.psa_attention_map_bwd(_ptr(do), _ptr(q), kv, _ptr(o), _ptr(lse), b, h, d, n_q, n_k, int(block), bm,
                                            bm_stride, scale, _ptr(dq), _ptr(dk), _ptr(dv), ws, nbytes,
-                                           _stream(None, q.device)))
+                                           _stream(None, q.device.index)))
     return dq, dk, dv

@@ -867,6 +867,12 @@ psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_
   a.row_order = (int32_t*)((char*)workspace + l.row_order);
   a.col_counts = (int32_t*)((char*)workspace + l.col_counts);
   a.col_order = (int32_t*)((char*)workspace + l.col_order);
+  a.part_q = (float*)((char*)workspace + l.part_q);
+  a.part_k = (float*)((char*)workspace + l.part_k);
+  a.part_v = (float*)((char*)workspace + l.part_v);
+  a.parts = l.parts;
+  a.head_parts = l.head_parts;
+  a.list_parts = l.list_parts;
   const hipError_t e = psa::launch_map_bwd(a, head_dim, stream);
   return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_attention_map_bwd launch");
 }

@@ -41,7 +41,9 @@ struct MapArgs {
   int32_t* paired;                    // whether pairs run (null: they do not)
   int32_t *col_counts, *col_order;    // backward: those of the (key head, key block) items
   int32_t n_bh, n_heads, group;       // group: query heads per key head
+  float *part_q, *part_k, *part_v;    // backward in parts: [item][parts][block][d]
   int32_t n_q, n_k, nbq, nbk, block, parts;
+  int32_t head_parts, list_parts;     // backward: parts of a key block's query heads, and of each one's list
   float c, scale;                     // scale log2(e), scale
 };
 struct MapLayout {
@@ -52,7 +54,8 @@ struct MapLayout {
 MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);
 struct MapBwdLayout {
-  size_t neg_lse2, neg_delta, row_counts, row_order, col_counts, col_order, total;  // (q_scaled first)
+  int32_t parts, head_parts, list_parts;
+  size_t neg_lse2, neg_delta, row_counts, row_order, col_counts, col_order, part_q, part_k, part_v, total;  // (q_scaled first)
 };
 MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t n_q, int32_t nbq, int32_t nbk,
                             int32_t block);

@@ -29,7 +29,7 @@
 namespace psa {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994530942f;
 
 // The kept entries of a row or column of the map (`len` bytes, `stride` apart), ascending, by all waves of the
 // workgroup.  Ends with a barrier.
@@ -353,6 +353,12 @@ __device__ __forceinline__ void store_cols(__bf16* dst, const f32x16& v, float f
   }
 }
 
+// The same, unscaled, into a part's fp32 sums.
+__device__ __forceinline__ void store_cols(float* dst, const f32x16& v) {
+#pragma unroll
+  for (int a = 0; a < 4; a++) *(f32x4*)(dst + 8 * a) = f32x4{v[4 * a], v[4 * a + 1], v[4 * a + 2], v[4 * a + 3]};
+}
+
 // ---------------------------------------------------------------------------------------------
 // Forward.
 // ---------------------------------------------------------------------------------------------
@@ -594,7 +600,9 @@ __global__ __launch_bounds__(256) void psa_mapped_rows_kernel(MapArgs a) {
   }
 }
 
-template <int D, int BLK>
+// SPLIT (here and for dk and dv): few blocks; `parts` workgroups share one, each takes a part of its list (dkv: of its
+// query heads first) and leaves its sums in the workspace, where psa_mapped_sum_kernel adds them.
+template <int D, int BLK, bool SPLIT>
 __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_dq_kernel(MapArgs a) {
   using T = Tile<D, BLK>;
   constexpr int HK = BLK / 2, W = 2 * T::kWaves, DH = T::DT / 2;
@@ -603,7 +611,8 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ int32_t found[W];
   extern __shared__ uint16_t list[];          // nbk entries
 
-  const int32_t item = a.row_order ? a.row_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
+  const int32_t whole = a.row_order ? a.row_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
+  const int32_t item = SPLIT ? whole / a.parts : whole, part = SPLIT ? whole - item * a.parts : 0;
   const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
   const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
@@ -613,8 +622,13 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int32_t n = a.n_k, n_q = a.n_q;
   const int row = qb * BLK + gw * 32 + r32;
 
-  const int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk, 1, a.nbk, list, found);
-  auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[i]); };
+  int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk, 1, a.nbk, list, found);
+  int32_t first = 0;
+  if constexpr (SPLIT) {
+    first = (int32_t)((int64_t)nu * part / a.parts);
+    nu = (int32_t)((int64_t)nu * (part + 1) / a.parts) - first;
+  }
+  auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[first + i]); };
   DmaPlan<D, BLK> plan;
   plan.init(__builtin_amdgcn_readfirstlane(wave), lane);
   int kb = 0;
@@ -685,8 +699,8 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
         out[(j * 4 + x) * 64][e] = grp == 0 ? dq[DH + j][4 * x + e] : dq[j][4 * x + e];
   __syncthreads();
   const f32x4* in = slot((1 - grp) * T::kWaves + gw);
-  if (row < n_q) {
-    __bf16* dst = a.dq + ((int64_t)bh * n_q + row) * D + 32 * DH * grp + 4 * h;
+  if (SPLIT || row < n_q) {
+    const int64_t dst = (SPLIT ? (int64_t)whole * BLK + gw * 32 + r32 : (int64_t)bh * n_q + row) * D + 32 * DH * grp + 4 * h;
 #pragma unroll
     for (int j = 0; j < DH; j++) {
       f32x16 v;
@@ -695,12 +709,15 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int e = 0; e < 4; e++)
           v[4 * x + e] = (grp == 0 ? dq[j][4 * x + e] : dq[DH + j][4 * x + e]) + in[(j * 4 + x) * 64][e];
-      store_cols(dst + 32 * j, v, a.scale);
+      if constexpr (SPLIT)
+        store_cols(a.part_q + dst + 32 * j, v);
+      else
+        store_cols(a.dq + dst + 32 * j, v, a.scale);
     }
   }
 }
 
-template <int D, int BLK>
+template <int D, int BLK, bool SPLIT>
 __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_dkv_kernel(MapArgs a) {
   using T = Tile<D, BLK>;
   constexpr int HQ = BLK / 2, W = 2 * T::kWaves;
@@ -710,7 +727,9 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ int32_t found[W];
   extern __shared__ uint16_t list[];          // nbq entries
 
-  const int32_t item = a.col_order ? a.col_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
+  const int32_t whole = a.col_order ? a.col_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
+  const int32_t parts = SPLIT ? a.head_parts * a.list_parts : 1;
+  const int32_t item = SPLIT ? whole / parts : whole, part = SPLIT ? whole - item * parts : 0;
   const int32_t bk = item / a.nbk, kb = item - bk * a.nbk, n_kv = a.n_heads / a.group;
   const int32_t b = bk / n_kv, hk = bk - b * n_kv;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
@@ -731,15 +750,24 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const Stream<D, BLK> stream(wave_s, lane);
   const LaneAt<D> at_lane(lane);
 
-  for (int32_t hd = hk * a.group; hd < (hk + 1) * a.group; hd++) {
+  // the query heads of this workgroup, and its part of each one's list
+  const int32_t hp = SPLIT ? part / a.list_parts : 0, lp = SPLIT ? part - hp * a.list_parts : 0;
+  const int32_t hd0 = hk * a.group + (SPLIT ? a.group * hp / a.head_parts : 0);
+  const int32_t hd1 = hk * a.group + (SPLIT ? a.group * (hp + 1) / a.head_parts : a.group);
+  for (int32_t hd = hd0; hd < hd1; hd++) {
     const int64_t bh = (int64_t)b * a.n_heads + hd;
     const __bf16 *qh = a.q_scaled + bh * n_q * D, *gh = a.grad_o + bh * n_q * D;
     // This wave's 64 of the 2 BLK row values of a block (waves behind them load none).
     const int part = wave_s * 64 / BLK, place = wave_s * 64 % BLK;
     const float* sh = (part == 0 ? a.neg_lse2 : a.neg_delta) + bh * a.nbq * BLK + place;
     // (its barriers also separate the buffers from the head before)
-    const int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + (int64_t)hd * a.nbq * a.nbk + kb, a.nbk, a.nbq, list, found);
-    auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[i]); };
+    int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + (int64_t)hd * a.nbq * a.nbk + kb, a.nbk, a.nbq, list, found);
+    int32_t first = 0;
+    if constexpr (SPLIT) {
+      first = (int32_t)((int64_t)nu * lp / a.list_parts);
+      nu = (int32_t)((int64_t)nu * (lp + 1) / a.list_parts) - first;
+    }
+    auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[first + i]); };
     auto issue = [&](int i) {
       const int qb = entry(i);
       stream.load(qh, lds_address(sq[i & 1]), qb, n_q);
@@ -794,8 +822,8 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
         out[(j * 4 + x) * 64][e] = grp == 0 ? dk[j][4 * x + e] : dv[j][4 * x + e];
   __syncthreads();
   const f32x4* in = slot((1 - grp) * T::kWaves + gw);
-  if (key < n_k) {
-    __bf16* dst = (grp == 0 ? a.dv : a.dk) + ((int64_t)bk * n_k + key) * D + 4 * h;
+  if (SPLIT || key < n_k) {
+    const int64_t dst = (SPLIT ? (int64_t)whole * BLK + gw * 32 + r32 : (int64_t)bk * n_k + key) * D + 4 * h;
 #pragma unroll
     for (int j = 0; j < T::DT; j++) {
       f32x16 t;
@@ -804,9 +832,41 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int e = 0; e < 4; e++)
           t[4 * x + e] = (grp == 0 ? dv[j][4 * x + e] : dk[j][4 * x + e]) + in[(j * 4 + x) * 64][e];
-      store_cols(dst + 32 * j, t, grp == 0 ? 1.0f : 0.69314718055994530942f);   // (scale q = ln 2 q')
+      if constexpr (SPLIT)
+        store_cols((grp == 0 ? a.part_v : a.part_k) + dst + 32 * j, t);
+      else
+        store_cols((grp == 0 ? a.dv : a.dk) + dst + 32 * j, t, grp == 0 ? 1.0f : kLn2);      // (scale q = ln 2 q')
     }
   }
+}
+
+// out = scale * the sum of the parts of every row, of up to two tensors alike.  D / 4 lanes a row.
+struct PartSums {
+  const float* part[2];
+  __bf16* out[2];
+  float scale[2];
+  int32_t heads, n, nb, parts;      // rows: `heads` x n, in nb blocks each
+};
+template <int D, int BLK>
+__global__ __launch_bounds__(256) void psa_mapped_sum_kernel(PartSums p) {
+  constexpr int L = D / 4;
+  const int64_t r = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  if (r >= (int64_t)p.heads * p.n) return;
+  const int c = threadIdx.x % L, which = blockIdx.y;
+  const int32_t head = (int32_t)(r / p.n), row = (int32_t)(r - (int64_t)head * p.n), blk = row / BLK;
+  const float* src = p.part[which] + (((int64_t)head * p.nb + blk) * p.parts * BLK + (row - blk * BLK)) * D + 4 * c;
+  f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = 0; i < p.parts; i++) s += *(const f32x4*)(src + (int64_t)i * BLK * D);
+  *(bf16x4*)(p.out[which] + r * D + 4 * c) = __builtin_convertvector(s * p.scale[which], bf16x4);
+}
+
+template <int D, int BLK>
+hipError_t launch_sums(const PartSums& p, int tensors, hipStream_t stream) {
+  const int64_t rows = (int64_t)p.heads * p.n;
+  hipLaunchKernelGGL((psa_mapped_sum_kernel<D, BLK>), dim3((uint32_t)((rows * (D / 4) + 255) / 256), tensors), dim3(256), 0,
+                     stream, p);
+  return hipGetLastError();
 }
 
 // Whether the items are more than the workgroups that run at once (one of 128 rows to a CU, two of 64).
@@ -827,10 +887,11 @@ hipError_t by_shape(int32_t head_dim, int32_t block, F f) {
 }  // namespace
 
 // Parts of every query block's list: as many as give every CU its workgroups where there are fewer query blocks
-// (two of 64 rows to a CU, one of 128), each part at least two blocks of a full row.
+// (two of 64 rows to a CU, one of 128), each part at least six blocks of a full row: the parts' sums cost a kernel more, 4 us,
+// and a block 0.5 to 1.3 us.
 int32_t map_parts(int32_t n_bh, int32_t nbq, int32_t nbk, int32_t block) {
   const int64_t items = (int64_t)n_bh * nbq, room = 256 * (128 / block);
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(room / items, nbk / 2));
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(room / items, nbk / 6));
 }
 
 MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
@@ -855,14 +916,26 @@ MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_
                             int32_t block) {
   const size_t rows = up256((size_t)n_bh * nbq * block * sizeof(float));
   const size_t q_items = up256((size_t)n_bh * nbq * sizeof(int32_t)), k_items = up256((size_t)n_kv * nbk * sizeof(int32_t));
+  const size_t tile = (size_t)block * head_dim * sizeof(float);
   MapBwdLayout l;
+  // dq's lists are shared out as the forward's; dk's and dv's over the query heads of a key head first
+  l.parts = map_parts(n_bh, nbq, nbk, block);
+  const int32_t group = n_bh / n_kv, room = std::max(1, (int32_t)(256 * (128 / block) / ((int64_t)n_kv * nbk)));
+  l.head_parts = std::min(group, room);
+  l.list_parts = std::max(1, std::min(room / l.head_parts, nbq / 6));
+  const int32_t kv_parts = l.head_parts * l.list_parts;
+  const size_t part_q = l.parts > 1 ? up256(tile * n_bh * nbq * l.parts) : 0;
+  const size_t part_kv = kv_parts > 1 ? up256(tile * n_kv * nbk * kv_parts) : 0;
   l.neg_lse2 = up256((size_t)n_bh * n_q * head_dim * sizeof(__bf16));
   l.neg_delta = l.neg_lse2 + rows;
   l.row_counts = l.neg_delta + rows;
   l.row_order = l.row_counts + q_items;
   l.col_counts = l.row_order + q_items;
   l.col_order = l.col_counts + k_items;
-  l.total = l.col_order + k_items;
+  l.part_q = l.col_order + k_items;
+  l.part_k = l.part_q + part_q;
+  l.part_v = l.part_k + part_kv;
+  l.total = l.part_v + part_kv;
   return l;
 }
 
@@ -923,12 +996,27 @@ hipError_t launch_map_bwd(const MapArgs& args, int32_t head_dim, hipStream_t str
     hipLaunchKernelGGL(psa_mapped_rows_kernel<D>, dim3((uint32_t)((rows * (D / 8) + 255) / 256)), dim3(256), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B>), dim3(a.n_bh / a.group * a.nbk), dim3(4 * B), list_bytes(a.nbq),
+    const int32_t n_kv = a.n_bh / a.group, kv_parts = a.head_parts * a.list_parts;
+    if (kv_parts == 1) {
+      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, false>), dim3(n_kv * a.nbk), dim3(4 * B), list_bytes(a.nbq), stream, a);
+      e = hipGetLastError();
+    } else {
+      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, true>), dim3(n_kv * a.nbk * kv_parts), dim3(4 * B), list_bytes(a.nbq),
+                         stream, a);
+      e = hipGetLastError();
+      if (e == hipSuccess)
+        e = launch_sums<D, B>({{a.part_k, a.part_v}, {a.dk, a.dv}, {kLn2, 1.0f}, n_kv, a.n_k, a.nbk, kv_parts}, 2, stream);
+    }
+    if (e != hipSuccess) return e;
+    if (a.parts == 1) {
+      hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B, false>), dim3(a.n_bh * a.nbq), dim3(4 * B), list_bytes(a.nbk), stream, a);
+      return hipGetLastError();
+    }
+    hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B, true>), dim3(a.n_bh * a.nbq * a.parts), dim3(4 * B), list_bytes(a.nbk),
                        stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B>), dim3(a.n_bh * a.nbq), dim3(4 * B), list_bytes(a.nbk), stream, a);
-    return hipGetLastError();
+    return launch_sums<D, B>({{a.part_q, nullptr}, {a.dq, nullptr}, {a.scale, 0.0f}, a.n_bh, a.n_q, a.nbq, a.parts}, 1, stream);
   });
 }
 
