@@ -418,8 +418,8 @@ psa_status_t psa_select_blocks(const void* q, const psa_kv_t* kv, int32_t batch,
 size_t psa_attention_map_workspace_size(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_q,
                                         int32_t n_k, int32_t block);
 
-/* Attention over a block map: o = softmax(scale * q k^T restricted to the kept tiles) v, numerics and empty rows
- * as psa_attention_fwd.
+/* Attention over a block map: o = softmax(scale * q k^T restricted to the kept tiles) v.  Numerics and empty rows
+ * as psa_attention_fwd, but for the scores: q is not rounded, the scale multiplies their fp32 sums.
  *   q, o         device bf16 [batch][n_heads][n_q][head_dim], 16-byte aligned
  *   blockmap     device uint8 [n_heads][nbq][nbk] per batch element, map_stride_b bytes from one to the next
  *                (0: the same map for all)
@@ -436,11 +436,10 @@ psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, i
 size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads,
                                             int32_t head_dim, int32_t n_q, int32_t n_k, int32_t block);
 
-/* Gradients of psa_attention_map_fwd.  Scores are formed again as the forward does (q scaled and rounded to bf16
- * once, also in dk; products summed in fp32), so that the weights are those of its lse; the weights and their
- * gradients are rounded to bf16 before the products that sum them, which are in fp32; dq, dk and dv are
- * rounded to bf16 once.  A shared key head's gradients are the sums over its query heads.
- * The order of every sum is fixed by the call's sizes and map.
+/* Gradients of psa_attention_map_fwd.  Scores are formed again, in fp32; the weights and their gradients are
+ * rounded to bf16 before the products that sum them, which are in fp32; dq, dk and dv are rounded to bf16
+ * once.  A shared key head's gradients are the sums over its query heads.  The order of every sum is fixed by
+ * the call's sizes and map.
  *   grad_o, o    device bf16 [batch][n_heads][n_q][head_dim]; o and lse as the forward left them
  *   dq           device bf16 [batch][n_heads][n_q][head_dim]: 0 for rows that keep nothing
  *   dk, dv       device bf16 [batch][kv->n_heads][n_k][head_dim], contiguous: 0 for keys that no row keeps

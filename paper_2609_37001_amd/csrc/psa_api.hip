@@ -401,7 +401,11 @@ psa_status_t check_map_call(const void* q, const psa_kv_t* kv, const void* o, co
   a->nbk = nbk;
   a->block = block;
   a->scale = softmax_scale;
-  a->c = softmax_scale * 1.4426950408889634f;
+  const double c = (double)softmax_scale * 1.4426950408889634;
+  a->c = (float)c;
+  int exponent = 1;
+  a->factor = c != 0.0 && std::isfinite(c) ? (float)(2.0 * std::frexp(std::fabs(c), &exponent)) : 1.0f;
+  a->pow2 = c != 0.0 && std::isfinite(c) ? (float)std::copysign(std::ldexp(1.0, exponent - 1), c) : (float)c;
   return PSA_OK;
 }
 
@@ -836,7 +840,7 @@ size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int3
   const SavedError keep;
   int32_t nbq, nbk;
   if (check_mapped(batch, n_heads, n_kv_heads, head_dim, n_q, n_k, block, &nbq, &nbk) != PSA_OK) return 0;
-  return psa::map_bwd_layout(batch * n_heads, batch * n_kv_heads, head_dim, n_q, nbq, nbk, block).total;
+  return psa::map_bwd_layout(batch * n_heads, batch * n_kv_heads, head_dim, nbq, nbk, block).total;
 }
 
 psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_kv_t* kv, const void* o,
@@ -853,15 +857,14 @@ psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_
   for (const void* p : {grad_o, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!p || !aligned(p, 16))
       return fail(PSA_ERR_INVALID, "grad_o, dq, dk and dv must be non-NULL and 16-byte aligned (%p)", p);
-  const psa::MapBwdLayout l = psa::map_bwd_layout(a.n_bh, batch * kv->n_heads, head_dim, n_q, a.nbq, a.nbk, block);
+  const psa::MapBwdLayout l = psa::map_bwd_layout(a.n_bh, batch * kv->n_heads, head_dim, a.nbq, a.nbk, block);
   s = check_map_workspace(workspace, workspace_bytes, l.total);
   if (s != PSA_OK) return s;
   a.grad_o = (const __bf16*)grad_o;
   a.dq = (__bf16*)dq;
   a.dk = (__bf16*)dk;
   a.dv = (__bf16*)dv;
-  a.q_scaled = (__bf16*)workspace;
-  a.neg_lse2 = (float*)((char*)workspace + l.neg_lse2);
+  a.neg_lse2 = (float*)workspace;
   a.neg_delta = (float*)((char*)workspace + l.neg_delta);
   a.row_counts = (int32_t*)((char*)workspace + l.row_counts);
   a.row_order = (int32_t*)((char*)workspace + l.row_order);

@@ -35,7 +35,6 @@ struct MapArgs {
   float* part_o;                      // forward in parts: [n_bh][nbq][parts][block][d] and (m, l) of the rows
   float2* part_ml;
   float *neg_lse2, *neg_delta;        // backward: [n_bh][nbq][block]
-  __bf16* q_scaled;                   // backward: bf16(scale log2(e) q), like q
   int32_t *row_counts, *row_order;    // list lengths of the (head, query block) items and their order
   int32_t *pair_counts, *pair_order;  // forward, block 64: those of pairs of query blocks, and
   int32_t* paired;                    // whether pairs run (null: they do not)
@@ -45,6 +44,7 @@ struct MapArgs {
   int32_t n_q, n_k, nbq, nbk, block, parts;
   int32_t head_parts, list_parts;     // backward: parts of a key block's query heads, and of each one's list
   float c, scale;                     // scale log2(e), scale
+  float pow2, factor;                 // forward: c = pow2 factor, a power of two with c's sign and a factor in [1, 2)
 };
 struct MapLayout {
   int32_t parts;
@@ -55,10 +55,9 @@ MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, i
 hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);
 struct MapBwdLayout {
   int32_t parts, head_parts, list_parts;
-  size_t neg_lse2, neg_delta, row_counts, row_order, col_counts, col_order, part_q, part_k, part_v, total;  // (q_scaled first)
+  size_t neg_delta, row_counts, row_order, col_counts, col_order, part_q, part_k, part_v, total;  // (neg_lse2 first)
 };
-MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t n_q, int32_t nbq, int32_t nbk,
-                            int32_t block);
+MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_bwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);
 
 }  // namespace psa

@@ -4,8 +4,11 @@
 //   backward  P = exp(S - lse), dP = do v^T, delta = rowsum(do * o), dS = P (dP - delta)
 //             dq = scale dS k,   dk = scale dS^T q,   dv = P^T do
 //
-// Both directions form S from the same operand, q' = bf16(scale log2(e) q), in the exp2 domain: whatever its
-// rounding does to the scores, the backward's weights are those of the forward's lse, and sum to 1.
+// Scores are exact up to their fp32 sums, in both directions: the forward scales q by a power of two alone (no
+// rounding) and multiplies every score by the rest of scale log2(e), a factor in [1, 2), before its exponential; the
+// backward multiplies by the whole.  Rounding scale log2(e) q to bf16 instead would save that multiplication (4 to 6 %
+// of the forward's time, 2 % of the backward's) and move scores by up to 2^-8 of the magnitudes they add: outputs
+// then are 2.9e-3 off instead of 2.35e-3, and a normaliser of rows whose scores share a large part by tenths.
 //
 // One workgroup takes one block of one side -- queries in the forward and for dq, keys for dk and dv -- holds its
 // rows in registers, and streams the blocks that the map keeps of the other side through LDS, double-buffered,
@@ -329,8 +332,8 @@ __device__ __forceinline__ void load_rows(bf16x8 (&y)[D / 16], const __bf16* row
   for (int cc = 0; cc < D / 16; cc++) y[cc] = *((const bf16x8*)row + h + 2 * cc);
 }
 
-// Where a tile's sums start: element e belongs to row 16 (e / 8) + e % 8 from `row` on.
-__device__ __forceinline__ f32x16 start_of(const float* row) {
+// A value for every row of a tile: element e belongs to row 16 (e / 8) + e % 8 from `row` on.
+__device__ __forceinline__ f32x16 row_values(const float* row) {
   f32x16 v;
 #pragma unroll
   for (int e = 0; e < 16; e++) v[e] = row[16 * (e >> 3) + (e & 7)];
@@ -411,7 +414,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
     load_rows<D>(st.q, a.q + ((int64_t)bh * n_q + min(row, n_q - 1)) * D, h);
 #pragma unroll
     for (int cc = 0; cc < T::DC; cc++)
-      st.q[cc] = __builtin_convertvector(__builtin_convertvector(st.q[cc], f32x8) * a.c, bf16x8);
+      st.q[cc] = __builtin_convertvector(__builtin_convertvector(st.q[cc], f32x8) * a.pow2, bf16x8);
 #pragma unroll
     for (int cc = 0; cc < T::DC; cc++) asm volatile("" ::"v"(st.q[cc]));
   }
@@ -437,7 +440,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
       f32x16 s[H::KT];
       qk_half<D, BLK, HK>(st, s, sk[i & 1], k0, lane);
       if (more) issue_block<D, BLK>(plan, vh, lds_address(sv[(i + 1) & 1]), kb, n);
-      softmax_pv_half<D, BLK, false, HK>(st, s, sv[i & 1], cur, k0, n, tail, ~0ull, ~0ull, lane, fresh);
+      softmax_pv_half<D, BLK, false, HK, true>(st, s, sv[i & 1], cur, k0, n, tail, ~0ull, ~0ull, lane, fresh, a.factor);
     } else if (more) {
       issue_block<D, BLK>(plan, vh, lds_address(sv[(i + 1) & 1]), kb, n);
     }
@@ -450,8 +453,8 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __syncthreads();                                        // (also: the buffers are no longer read)
   const float2 other = stat[(1 - grp) * T::kWaves + gw][r32];
   const float top = fmaxf(st.m, other.x);
-  const float alpha = st.m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(st.m - top);
-  const float beta = other.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(other.x - top);
+  const float alpha = st.m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((st.m - top) * a.factor);
+  const float beta = other.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((other.x - top) * a.factor);
   const float lsum = mine * alpha + other.y * beta;
   const float inv = SPLIT ? 1.0f : lsum > 0.0f ? 1.0f / lsum : 0.0f;
   static_assert(W * DH * 4096 <= 4 * T::BYTES, "a wave's half of O fits its share of the buffers");
@@ -490,7 +493,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
     if constexpr (SPLIT)
       a.part_ml[place] = make_float2(top, lsum);
     else if (a.lse)
-      a.lse[place] = lsum > 0.0f ? (top + __builtin_log2f(lsum)) * 0.69314718055994530942f : -__builtin_inff();
+      a.lse[place] = lsum > 0.0f ? (top * a.factor + __builtin_log2f(lsum)) * kLn2 : -__builtin_inff();
   }
 }
 
@@ -535,13 +538,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4
   DmaPlan<D, BLK> plan;
   plan.init(__builtin_amdgcn_readfirstlane(wave), lane);
   const int64_t kv_off = b * a.kv_stride_b + (hd / a.group) * a.kv_stride_h, off = (int64_t)bh * a.n_q;
-  process_pair<D, BLK, 1, true, false>(plan, grp, a.q + off * D, a.k + kv_off, a.v + kv_off, a.o + off * D,
+  process_pair<D, BLK, 1, true, false, true>(plan, grp, a.q + off * D, a.k + kv_off, a.v + kv_off, a.o + off * D,
                                        a.lse ? a.lse + off : nullptr, a.n_q, a.n_k,
-                                       __builtin_amdgcn_readfirstlane(grp == 0 ? pr.x : pr.y), nu, 0, list, a.c, sk, sv,
-                                       nullptr);
+                                       __builtin_amdgcn_readfirstlane(grp == 0 ? pr.x : pr.y), nu, 0, list, a.pow2, sk, sv,
+                                       nullptr, a.factor);
 }
 
-// Adds the parts of every query row: o = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p.  D / 4 lanes a row.
+// Adds the parts of every query row: o = sum_p 2^(f (m_p - m)) O_p / sum_p 2^(f (m_p - m)) l_p.  D / 4 lanes a row.
 template <int D, int BLK>
 __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
   constexpr int L = D / 4;
@@ -558,22 +561,21 @@ __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
   for (int p = 0; p < a.parts; p++) {
     const int64_t at = first + (int64_t)p * BLK;
     const float2 ml = a.part_ml[at];
-    const float w = ml.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
+    const float w = ml.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((ml.x - m) * a.factor);
     l += w * ml.y;
     o += *(const f32x4*)(a.part_o + at * D + 4 * c) * w;
   }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
   *(bf16x4*)(a.o + r * D + 4 * c) = __builtin_convertvector(o * inv, bf16x4);
-  if (a.lse && c == 0) a.lse[r] = l > 0.0f ? (m + __builtin_log2f(l)) * 0.69314718055994530942f : -__builtin_inff();
+  if (a.lse && c == 0) a.lse[r] = l > 0.0f ? (m * a.factor + __builtin_log2f(l)) * kLn2 : -__builtin_inff();
 }
 
 // ---------------------------------------------------------------------------------------------
 // Backward.
 // ---------------------------------------------------------------------------------------------
 
-// Per query row, in blocks of `block` rows: -lse log2(e) and -delta, where the sums of S and dP start; and q'.  Rows
-// behind the last one, and rows that keep nothing (lse = -inf), get -inf: every weight formed with it is 0.
-// D / 8 lanes a row.
+// Per query row, in blocks of `block` rows: -lse log2(e), and -delta, where the sums of dP start.  Rows behind the last
+// one, and rows that keep nothing (lse = -inf), get -inf: every weight formed with it is 0.  D / 8 lanes a row.
 template <int D>
 __global__ __launch_bounds__(256) void psa_mapped_rows_kernel(MapArgs a) {
   constexpr int L = D / 8;
@@ -585,13 +587,11 @@ __global__ __launch_bounds__(256) void psa_mapped_rows_kernel(MapArgs a) {
   const int64_t at = (int64_t)bh * a.n_q + min(row, a.n_q - 1);
   const f32x8 x = __builtin_convertvector(*(const bf16x8*)(a.grad_o + at * D + 8 * c), f32x8);
   const f32x8 y = __builtin_convertvector(*(const bf16x8*)(a.o + at * D + 8 * c), f32x8);
-  const f32x8 q = __builtin_convertvector(*(const bf16x8*)(a.q + at * D + 8 * c), f32x8);
   float s = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; e++) s = fmaf(x[e], y[e], s);
 #pragma unroll
   for (int off = L / 2; off > 0; off >>= 1) s += __shfl_xor(s, off);
-  if (row < a.n_q) *(bf16x8*)(a.q_scaled + at * D + 8 * c) = __builtin_convertvector(q * a.c, bf16x8);
   if (c == 0) {
     const float lse = a.lse[at];
     const bool none = row >= a.n_q || lse == -__builtin_inff();
@@ -640,7 +640,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const LaneAt<D> at_lane(lane);
   bf16x8 q[T::DC], g[T::DC];
   const int64_t at = ((int64_t)bh * n_q + min(row, n_q - 1)) * D;
-  load_rows<D>(q, a.q_scaled + at, h);
+  load_rows<D>(q, a.q + at, h);
   load_rows<D>(g, a.grad_o + at, h);
   const int64_t sat = (int64_t)bh * a.nbq * BLK + row;
   const float neg_lse2 = a.neg_lse2[sat], neg_delta = a.neg_delta[sat];
@@ -665,7 +665,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int kt = 0; kt < HK / 32; kt++) {
       const int k0 = grp * HK + 32 * kt;
-      f32x16 s = rows_times<D>(q, kr + 32 * kt * T::RB, (f32x16){} + neg_lse2);
+      f32x16 s = rows_times<D>(q, kr + 32 * kt * T::RB, (f32x16){});
       f32x16 dp = rows_times<D>(g, vr + 32 * kt * T::RB, (f32x16){} + neg_delta);
       if (tail) {
         // Keys behind the last one read as the last one, whose weight is finite: no gradient of theirs.
@@ -676,7 +676,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
           if (kbase + 16 * (e >> 3) + (e & 7) >= n) dp[e] = 0.0f;
       }
 #pragma unroll
-      for (int e = 0; e < 16; e++) dp[e] *= __builtin_amdgcn_exp2f(s[e]);
+      for (int e = 0; e < 16; e++) dp[e] *= __builtin_amdgcn_exp2f(fmaf(s[e], a.c, neg_lse2));
 #pragma unroll
       for (int j = 0; j < 2; j++) {
         const int off = (32 * kt + 16 * j) * T::RB;
@@ -756,7 +756,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int32_t hd1 = hk * a.group + (SPLIT ? a.group * (hp + 1) / a.head_parts : a.group);
   for (int32_t hd = hd0; hd < hd1; hd++) {
     const int64_t bh = (int64_t)b * a.n_heads + hd;
-    const __bf16 *qh = a.q_scaled + bh * n_q * D, *gh = a.grad_o + bh * n_q * D;
+    const __bf16 *qh = a.q + bh * n_q * D, *gh = a.grad_o + bh * n_q * D;
     // This wave's 64 of the 2 BLK row values of a block (waves behind them load none).
     const int part = wave_s * 64 / BLK, place = wave_s * 64 % BLK;
     const float* sh = (part == 0 ? a.neg_lse2 : a.neg_delta) + bh * a.nbq * BLK + place;
@@ -788,10 +788,11 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
       for (int kt = 0; kt < HQ / 32; kt++) {
         const int q0 = grp * HQ + 32 * kt;
         __builtin_amdgcn_sched_barrier(0);      // one tile's operands at a time
-        f32x16 s = rows_times<D>(k, qr + 32 * kt * T::RB, start_of(&stat[i & 1][0][q0 + 8 * h]));
-        f32x16 dp = rows_times<D>(v, gr + 32 * kt * T::RB, start_of(&stat[i & 1][1][q0 + 8 * h]));
+        f32x16 s = rows_times<D>(k, qr + 32 * kt * T::RB, (f32x16){});
+        f32x16 dp = rows_times<D>(v, gr + 32 * kt * T::RB, row_values(&stat[i & 1][1][q0 + 8 * h]));
+        const f32x16 neg_lse2 = row_values(&stat[i & 1][0][q0 + 8 * h]);
 #pragma unroll
-        for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(s[e]);
+        for (int e = 0; e < 16; e++) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.c, neg_lse2[e]));
 #pragma unroll
         for (int j = 0; j < 2; j++) {
           const int off = (32 * kt + 16 * j) * T::RB;
@@ -835,7 +836,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
       if constexpr (SPLIT)
         store_cols((grp == 0 ? a.part_v : a.part_k) + dst + 32 * j, t);
       else
-        store_cols((grp == 0 ? a.dv : a.dk) + dst + 32 * j, t, grp == 0 ? 1.0f : kLn2);      // (scale q = ln 2 q')
+        store_cols((grp == 0 ? a.dv : a.dk) + dst + 32 * j, t, grp == 0 ? 1.0f : a.scale);
     }
   }
 }
@@ -912,8 +913,7 @@ MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, i
   return l;
 }
 
-MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t n_q, int32_t nbq, int32_t nbk,
-                            int32_t block) {
+MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
   const size_t rows = up256((size_t)n_bh * nbq * block * sizeof(float));
   const size_t q_items = up256((size_t)n_bh * nbq * sizeof(int32_t)), k_items = up256((size_t)n_kv * nbk * sizeof(int32_t));
   const size_t tile = (size_t)block * head_dim * sizeof(float);
@@ -926,8 +926,7 @@ MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_
   const int32_t kv_parts = l.head_parts * l.list_parts;
   const size_t part_q = l.parts > 1 ? up256(tile * n_bh * nbq * l.parts) : 0;
   const size_t part_kv = kv_parts > 1 ? up256(tile * n_kv * nbk * kv_parts) : 0;
-  l.neg_lse2 = up256((size_t)n_bh * n_q * head_dim * sizeof(__bf16));
-  l.neg_delta = l.neg_lse2 + rows;
+  l.neg_delta = rows;
   l.row_counts = l.neg_delta + rows;
   l.row_order = l.row_counts + q_items;
   l.col_counts = l.row_order + q_items;
@@ -1005,7 +1004,7 @@ hipError_t launch_map_bwd(const MapArgs& args, int32_t head_dim, hipStream_t str
                          stream, a);
       e = hipGetLastError();
       if (e == hipSuccess)
-        e = launch_sums<D, B>({{a.part_k, a.part_v}, {a.dk, a.dv}, {kLn2, 1.0f}, n_kv, a.n_k, a.nbk, kv_parts}, 2, stream);
+        e = launch_sums<D, B>({{a.part_k, a.part_v}, {a.dk, a.dv}, {a.scale, 1.0f}, n_kv, a.n_k, a.nbk, kv_parts}, 2, stream);
     }
     if (e != hipSuccess) return e;
     if (a.parts == 1) {

@@ -182,14 +182,19 @@ __device__ __forceinline__ void qk_half(const WaveState<D, BLK>& st,
 //  * Masked keys: past the sequence end (one-dimensional blocks: only the last block), or, in
 //    the PSABlock-centric layout (PAD), every position whose bit in the tile's validity words
 //    (lo: positions 0..63, hi: 64..127) is clear -- 3D padding and the end of the sequence.
-template <int D, int BLK, bool PAD, int HK = 64>
+//  * FACTOR: the scores are in units of log2 of a weight divided by `factor`, in [1, 2), and so are the base and
+//    st.m: a weight is 2^(factor (S - base)).  q then needs scaling by a power of two alone, which rounds nothing,
+//    for one multiplication a score.  (The base moves when a score is 4 above it, at head dim 64 when a weight
+//    reaches 2, then to 3 above the maximum.)
+template <int D, int BLK, bool PAD, int HK = 64, bool FACTOR = false>
 __device__ __forceinline__ void softmax_pv_half(WaveState<D, BLK>& st,
                                                 f32x16 (&s)[Half<D, BLK, HK>::KT], const uint8_t* sv,
                                                 int kb, int k0, int n, bool tail, uint64_t lo,
-                                                uint64_t hi, int lane, int& fresh) {
+                                                uint64_t hi, int lane, int& fresh, float factor = 1.0f) {
   using T = Tile<D, BLK>;
   using H = Half<D, BLK, HK>;
   const int h = lane >> 5, g = lane >> 4, j16 = lane & 15;
+  auto pow2 = [&](float x) { return __builtin_amdgcn_exp2f(FACTOR ? x * factor : x); };
   if (tail) {
     asm volatile("" ::: "memory");        // keep the mask a branch taken only by partial tiles
     int hh = h;
@@ -249,7 +254,7 @@ __device__ __forceinline__ void softmax_pv_half(WaveState<D, BLK>& st,
       for (int j = 0; j < H::KC; j++) {
         f32x8 e;
 #pragma unroll
-        for (int x = 0; x < 8; x++) e[x] = __builtin_amdgcn_exp2f(s[j >> 1][8 * (j & 1) + x]);
+        for (int x = 0; x < 8; x++) e[x] = pow2(s[j >> 1][8 * (j & 1) + x]);
         p[j] = __builtin_convertvector(e, bf16x8);
       }
     };
@@ -272,8 +277,8 @@ __device__ __forceinline__ void softmax_pv_half(WaveState<D, BLK>& st,
       const float base = st.base();
       const float ms = pair_max(mx) + base;
       const bool need = ms > st.m + 0.5f;
-      const float up = ms + 6.0f;
-      const float alpha = need ? __builtin_amdgcn_exp2f(st.m - up) : 1.0f;
+      const float up = ms + (FACTOR ? 3.0f : 6.0f);
+      const float alpha = need ? pow2(st.m - up) : 1.0f;
       const float shift = need ? up - base : 0.0f;
       st.m = need ? up : st.m;
       st.l *= alpha;
@@ -308,10 +313,10 @@ __device__ __forceinline__ void softmax_pv_half(WaveState<D, BLK>& st,
     const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
     const float base = st.base();
     const float ms = pair_max(mx) + base;
-    const bool need = ms - st.m > 8.0f;     // false for -inf - -inf (NaN)
+    const bool need = ms - st.m > (FACTOR ? 4.0f : 8.0f);     // false for -inf - -inf (NaN)
     if (__builtin_amdgcn_ballot_w64(need)) {
       asm volatile("" ::: "memory");        // keep this rare path a branch
-      const float alpha = need ? __builtin_amdgcn_exp2f(st.m - ms) : 1.0f;
+      const float alpha = need ? pow2(st.m - ms) : 1.0f;
       const float shift = need ? ms - base : 0.0f;
       st.m = need ? ms : st.m;
       st.l *= alpha;
@@ -344,7 +349,7 @@ __device__ __forceinline__ void softmax_pv_half(WaveState<D, BLK>& st,
       __builtin_amdgcn_sched_barrier(0);      // keep the reads ahead of the exponentials
       f32x8 e;
 #pragma unroll
-      for (int x = 0; x < 8; x++) e[x] = __builtin_amdgcn_exp2f(s[j >> 1][8 * (j & 1) + x]);
+      for (int x = 0; x < 8; x++) e[x] = pow2(s[j >> 1][8 * (j & 1) + x]);
       const bf16x8 p = __builtin_convertvector(e, bf16x8);
       // Row sum of the rounded weights, two per instruction: the normaliser matches the P that
       // multiplies V.
@@ -443,10 +448,11 @@ __device__ __forceinline__ void store_rows(const WaveState<D, BLK>& st, __bf16* 
 // no other wave touches; 16-byte chunks XOR-swizzled by the row), then stored as whole rows, 16
 // bytes per lane, so that each store covers 64 x 16 contiguous bytes of O instead of 8 bytes in
 // each of 32 rows.  row0 = the wave's first row; lane l holds row row0 + (l & 31).
-template <int D, int BLK>
+// (m times `factor`: in log2 units; 1 without a factor.)
+template <int D, int BLK, bool FACTOR = false>
 __device__ __forceinline__ void store_rows_staged(const WaveState<D, BLK>& st, __bf16* __restrict__ oh,
                                                   float* __restrict__ lseh, int row0, int n, int lane,
-                                                  uint32_t stage) {
+                                                  uint32_t stage, float factor = 1.0f) {
   using T = Tile<D, BLK>;
   constexpr int RB = 2 * D;                   // bytes per row
   constexpr int C16 = RB / 16;                // 16-byte chunks per row
@@ -472,7 +478,7 @@ __device__ __forceinline__ void store_rows_staged(const WaveState<D, BLK>& st, _
     if (row0 + rr < n) *(u32x4*)(oh + (size_t)(row0 + rr) * D + 8 * c) = val;
   }
   if (lseh && h == 0 && row0 + r < n)
-    lseh[row0 + r] = lsum > 0.0f ? (st.m + __builtin_log2f(lsum)) * 0.69314718055994530942f
+    lseh[row0 + r] = lsum > 0.0f ? ((FACTOR ? st.m * factor : st.m) + __builtin_log2f(lsum)) * 0.69314718055994530942f
                                  : -__builtin_inff();
 }
 
@@ -487,7 +493,9 @@ static_assert(PSA_MAX_BLOCKS <= (1 << kEntryRowShift), "block index fits the ent
 // Block i sits in buffer i & 1; after one barrier (its loads, issued a block earlier, have landed
 // and block i - 1 is no longer read) the loads of block i + 1 go out and each row that keeps block
 // i runs it: Q K^T, softmax and P V for each step of 64 keys.
-template <int D, int BLK, int SUB, bool SPARSE, bool PAD>
+// FACTOR: c is the power of two (with a sign, or 0) that q is scaled by, `factor` that of the scores, see
+// softmax_pv_half.
+template <int D, int BLK, int SUB, bool SPARSE, bool PAD, bool FACTOR = false>
 __device__ __forceinline__ void process_pair(const DmaPlan<D, BLK>& plan, int grp,
                                              const __bf16* __restrict__ qh,
                                              const __bf16* __restrict__ kh,
@@ -497,7 +505,7 @@ __device__ __forceinline__ void process_pair(const DmaPlan<D, BLK>& plan, int gr
                                              const uint16_t* list, float c,
                                              uint8_t (*sk)[Tile<D, BLK>::BYTES],
                                              uint8_t (*sv)[Tile<D, BLK>::BYTES],
-                                             const uint64_t* masks) {
+                                             const uint64_t* masks, float factor = 1.0f) {
   using T = Tile<D, BLK>;
   using H = Half<D, BLK>;
   const int tid = threadIdx.x, lane = tid & 63, gw = (tid >> 6) & (T::kWaves - 1);
@@ -601,10 +609,10 @@ __device__ __forceinline__ void process_pair(const DmaPlan<D, BLK>& plan, int gr
       f32x16 s[H::KT];
       qk_half<D, BLK>(st, s, skb, 0, lane);
       if (more) issue_v((i + 1) & 1, kbn);
-      softmax_pv_half<D, BLK, PAD>(st, s, svb, kb, 0, n, tail, lo, hi, lane, fresh);
+      softmax_pv_half<D, BLK, PAD, 64, FACTOR>(st, s, svb, kb, 0, n, tail, lo, hi, lane, fresh, factor);
       if constexpr (BLK > H::HK) {
         qk_half<D, BLK>(st, s, skb, H::HK, lane);
-        softmax_pv_half<D, BLK, PAD>(st, s, svb, kb, H::HK, n, tail, lo, hi, lane, fresh);
+        softmax_pv_half<D, BLK, PAD, 64, FACTOR>(st, s, svb, kb, H::HK, n, tail, lo, hi, lane, fresh, factor);
       }
     } else if (more) {
       issue_v((i + 1) & 1, kbn);
@@ -616,7 +624,7 @@ __device__ __forceinline__ void process_pair(const DmaPlan<D, BLK>& plan, int gr
     if (my_row >= 0) {
       static_assert(T::kWaves * 32 * 2 * D <= T::BYTES, "a wave's rows fit its share of a free buffer");
       const uint32_t stage = lds_address(grp == 0 ? sk[nu & 1] : sv[nu & 1]) + gw * (32 * 2 * D);
-      store_rows_staged<D, BLK>(st, oh, lseh, my_row * BLK + gw * 32, n_q, lane, stage);
+      store_rows_staged<D, BLK, FACTOR>(st, oh, lseh, my_row * BLK + gw * 32, n_q, lane, stage, factor);
     }
   } else {
     if (my_row >= 0) store_rows<D, BLK>(st, oh, lseh, row, n_q, lane);
