@@ -34,28 +34,31 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994530942f;
 
-// The kept entries of a row or column of the map (`len` bytes, `stride` apart), ascending, by all waves of the
-// workgroup.  Ends with a barrier.
-template <int W>
-__device__ __forceinline__ int32_t kept_list(const uint8_t* __restrict__ row, int64_t stride, int32_t len,
-                                             uint16_t* list, int32_t* found) {
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  int32_t nu = 0;
-  for (int32_t base = 0; base < len; base += W * 64) {
-    const int32_t i = base + tid;
-    const bool keep = i < len && row[i * stride] != 0;
-    const uint64_t mask = __builtin_amdgcn_ballot_w64(keep);
-    if (lane == 0) found[wave] = __builtin_popcountll(mask);
-    __syncthreads();
-    int32_t pos = nu;
+// The kept entries of `len` places, ascending, by all waves of the workgroup: entry(i) is what to list for place i, -1
+// for nothing.  Each wave counts a run of the places and, once all counts are known, goes over it again: two
+// barriers for any length.  Ends with a barrier.
+template <int W, typename F>
+__device__ __forceinline__ int32_t kept_list(int32_t len, uint16_t* list, int32_t* found, F entry) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int32_t run = (len + W * 64 - 1) / (W * 64) * 64, i0 = wave * run, i1 = min(len, i0 + run);
+  int32_t mine = 0;
+  for (int32_t i = i0; i < i1; i += 64)
+    mine += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < i1 && entry(i + lane) >= 0));
+  if (lane == 0) found[wave] = mine;
+  __syncthreads();
+  int32_t pos = 0, nu = 0;
 #pragma unroll
-    for (int w = 0; w < W; w++) {
-      pos += w < wave ? found[w] : 0;
-      nu += found[w];
-    }
-    if (keep) list[pos + __builtin_popcountll(mask & ((1ull << lane) - 1))] = (uint16_t)i;
-    __syncthreads();
+  for (int w = 0; w < W; w++) {
+    pos += w < wave ? found[w] : 0;
+    nu += found[w];
   }
+  for (int32_t i = i0; i < i1; i += 64) {
+    const int32_t e = i + lane < i1 ? entry(i + lane) : -1;
+    const uint64_t mask = __builtin_amdgcn_ballot_w64(e >= 0);
+    if (e >= 0) list[pos + __builtin_popcountll(mask & ((1ull << lane) - 1))] = (uint16_t)e;
+    pos += __builtin_popcountll(mask);
+  }
+  __syncthreads();
   return __builtin_amdgcn_readfirstlane(nu);
 }
 
@@ -393,7 +396,8 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // whether any of this wave's rows exists
   const bool rows = __builtin_amdgcn_readfirstlane(qb * BLK + gw * 32) < n_q;
 
-  int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk, 1, a.nbk, list, found);
+  const uint8_t* kept = a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk;
+  int32_t nu = kept_list<W>(a.nbk, list, found, [&](int32_t i) { return kept[i] ? i : -1; });
   int32_t first = 0;
   if constexpr (SPLIT) {
     first = (int32_t)((int64_t)nu * part / a.parts);
@@ -516,25 +520,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
   const uint8_t* first = a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + pr.x) * a.nbk;
-  int32_t nu = 0;
-  for (int32_t base = 0; base < a.nbk; base += W * 64) {
-    const int32_t kb = base + tid;
-    const bool x = kb < a.nbk && first[kb] != 0, y = kb < a.nbk && pr.y >= 0 && first[(int64_t)a.nbk + kb] != 0;
-    const uint64_t mask = __builtin_amdgcn_ballot_w64(x || y);
-    if (lane == 0) found[wave] = __builtin_popcountll(mask);
-    __syncthreads();
-    int32_t pos = nu;
-#pragma unroll
-    for (int w = 0; w < W; w++) {
-      pos += w < wave ? found[w] : 0;
-      nu += found[w];
-    }
-    if (x || y)
-      list[pos + __builtin_popcountll(mask & ((1ull << lane) - 1))] =
-          (uint16_t)(kb | (x ? 1 << kEntryRowShift : 0) | (y ? 2 << kEntryRowShift : 0));
-    __syncthreads();
-  }
-  nu = __builtin_amdgcn_readfirstlane(nu);
+  const int32_t nu = kept_list<W>(a.nbk, list, found, [&](int32_t i) {
+    const int rows = (first[i] ? 1 : 0) | (pr.y >= 0 && first[(int64_t)a.nbk + i] ? 2 : 0);
+    return rows ? i | rows << kEntryRowShift : -1;
+  });
   DmaPlan<D, BLK> plan;
   plan.init(__builtin_amdgcn_readfirstlane(wave), lane);
   const int64_t kv_off = b * a.kv_stride_b + (hd / a.group) * a.kv_stride_h, off = (int64_t)bh * a.n_q;
@@ -544,26 +533,43 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4
                                        nullptr, a.factor);
 }
 
-// Adds the parts of every query row: o = sum_p 2^(f (m_p - m)) O_p / sum_p 2^(f (m_p - m)) l_p.  D / 4 lanes a row.
-template <int D, int BLK>
+// Adds the parts of a query row: o = sum_p 2^(f (m_p - m)) O_p / sum_p 2^(f (m_p - m)) l_p.  D / 4 lanes for a row's
+// channels, G of these side by side for its parts: one where parts are few and rows many (10400 rows in three parts:
+// 4 us less than with a workgroup a row), else all 256 / (D / 4) of a workgroup (one lane for all 64 parts of
+// a single token took 15 us).
+template <int D, int BLK, int G>
 __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
-  constexpr int L = D / 4;
-  const int64_t r = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  constexpr int L = D / 4, R = 256 / (L * G);
+  __shared__ f32x4 sum_o[G > 1 ? G : 1][L];
+  __shared__ float2 sum_ml[G];
+  const int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / (L * G);
   if (r >= (int64_t)a.n_bh * a.n_q) return;
-  const int c = threadIdx.x % L;
+  const int c = threadIdx.x % L, g = threadIdx.x / L % G;
   const int32_t bh = (int32_t)(r / a.n_q), row = (int32_t)(r - (int64_t)bh * a.n_q), qb = row / BLK;
   const int64_t first = ((int64_t)bh * a.nbq + qb) * a.parts * BLK + (row - qb * BLK);
-  float m = -__builtin_inff();
-  for (int p = 0; p < a.parts; p++) m = fmaxf(m, a.part_ml[first + (int64_t)p * BLK].x);
+  float m = -__builtin_inff(), l = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  float l = 0.0f;
+  auto add = [&](float pm, float pl, f32x4 po) {
+    const float top = fmaxf(m, pm);
+    const float was = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - top) * a.factor);
+    const float w = pm == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((pm - top) * a.factor);
+    l = l * was + pl * w;
+    o = o * was + po * w;
+    m = top;
+  };
 #pragma unroll 4
-  for (int p = 0; p < a.parts; p++) {
+  for (int p = g; p < a.parts; p += G) {
     const int64_t at = first + (int64_t)p * BLK;
     const float2 ml = a.part_ml[at];
-    const float w = ml.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((ml.x - m) * a.factor);
-    l += w * ml.y;
-    o += *(const f32x4*)(a.part_o + at * D + 4 * c) * w;
+    add(ml.x, ml.y, *(const f32x4*)(a.part_o + at * D + 4 * c));
+  }
+  if constexpr (G > 1) {
+    sum_o[g][c] = o;
+    if (c == 0) sum_ml[g] = make_float2(m, l);
+    __syncthreads();
+    if (g > 0) return;
+#pragma unroll
+    for (int i = 1; i < G; i++) add(sum_ml[i].x, sum_ml[i].y, sum_o[i][c]);
   }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
   *(bf16x4*)(a.o + r * D + 4 * c) = __builtin_convertvector(o * inv, bf16x4);
@@ -622,7 +628,8 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int32_t n = a.n_k, n_q = a.n_q;
   const int row = qb * BLK + gw * 32 + r32;
 
-  int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk, 1, a.nbk, list, found);
+  const uint8_t* kept = a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk;
+  int32_t nu = kept_list<W>(a.nbk, list, found, [&](int32_t i) { return kept[i] ? i : -1; });
   int32_t first = 0;
   if constexpr (SPLIT) {
     first = (int32_t)((int64_t)nu * part / a.parts);
@@ -761,7 +768,8 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const int part = wave_s * 64 / BLK, place = wave_s * 64 % BLK;
     const float* sh = (part == 0 ? a.neg_lse2 : a.neg_delta) + bh * a.nbq * BLK + place;
     // (its barriers also separate the buffers from the head before)
-    int32_t nu = kept_list<W>(a.map + b * a.map_stride_b + (int64_t)hd * a.nbq * a.nbk + kb, a.nbk, a.nbq, list, found);
+    const uint8_t* kept = a.map + b * a.map_stride_b + (int64_t)hd * a.nbq * a.nbk + kb;
+    int32_t nu = kept_list<W>(a.nbq, list, found, [&](int32_t i) { return kept[(int64_t)i * a.nbk] ? i : -1; });
     int32_t first = 0;
     if constexpr (SPLIT) {
       first = (int32_t)((int64_t)nu * lp / a.list_parts);
@@ -979,8 +987,12 @@ hipError_t launch_map_fwd(const MapArgs& args, int32_t head_dim, hipStream_t str
     hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, true>), grid, dim3(4 * B), list_bytes(a.nbk), stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t rows = (int64_t)a.n_bh * a.n_q;
-    hipLaunchKernelGGL((psa_mapped_join_kernel<D, B>), dim3((uint32_t)((rows * (D / 4) + 255) / 256)), dim3(256), 0, stream, a);
+    constexpr int kLanes = D / 4, kSide = 256 / kLanes;
+    const int32_t rows = a.n_bh * a.n_q;
+    if (a.parts <= 4)
+      hipLaunchKernelGGL((psa_mapped_join_kernel<D, B, 1>), dim3((rows + kSide - 1) / kSide), dim3(256), 0, stream, a);
+    else
+      hipLaunchKernelGGL((psa_mapped_join_kernel<D, B, kSide>), dim3(rows), dim3(256), 0, stream, a);
     return hipGetLastError();
   });
 }
