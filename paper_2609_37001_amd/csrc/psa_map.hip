@@ -145,13 +145,16 @@ __global__ __launch_bounds__(256) void psa_mapped_col_count_kernel(MapArgs a) {
   if (wave == 0 && kb < a.nbk) a.col_counts[bk * a.nbk + kb] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
 }
 
+constexpr int kOrderThreads = 1024, kOrderClasses = 8, kOrderRun = 8;
+
 // Sum of a list over the workgroup, in every thread.
 __device__ __forceinline__ unsigned long long list_sum(const int32_t* counts, int32_t n, unsigned long long* total) {
   __syncthreads();
   if (threadIdx.x == 0) *total = 0;
   __syncthreads();
   unsigned long long mine = 0;
-  for (int32_t i = threadIdx.x; i < n; i += blockDim.x) mine += counts[i];
+#pragma unroll 8
+  for (int32_t i = threadIdx.x; i < n; i += kOrderThreads) mine += counts[i];
   atomicAdd(total, mine);
   __syncthreads();
   return *total;
@@ -160,7 +163,6 @@ __device__ __forceinline__ unsigned long long list_sum(const int32_t* counts, in
 // order[workgroup] = item: eight classes of list lengths around the mean, longest first, each in the items' order and
 // spread over the XCDs.  One workgroup per list of items; each thread takes a run of them.  Pairs' lists come second:
 // their workgroup also says whether they pay (pairs_pay).
-constexpr int kOrderThreads = 1024, kOrderClasses = 8;
 struct OrderList {
   const int32_t* counts;
   int32_t* order;
@@ -187,12 +189,23 @@ __global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(OrderLi
     return x >= 4.0f * mean ? 0 : x >= 2.83f * mean ? 1 : x >= 2.0f * mean ? 2 : x >= 1.5f * mean ? 3 :
            x >= 1.25f * mean ? 4 : x >= 1.1f * mean ? 5 : x >= 0.9f * mean ? 6 : 7;
   };
+  // A thread's items in runs of kOrderRun, whose counts are read at once (one after the other their latencies were
+  // most of the kernel: 20 us for 8896 items).
+  auto each_item = [&](auto f) {
+    for (int32_t i = i0; i < i1; i += kOrderRun) {
+      int32_t c[kOrderRun];
+#pragma unroll
+      for (int u = 0; u < kOrderRun; u++) c[u] = counts[min(i + u, n - 1)];
+#pragma unroll
+      for (int u = 0; u < kOrderRun; u++)
+        if (i + u < i1) f(i + u, cls(c[u]));
+    }
+  };
   int32_t have[kOrderClasses] = {};
-  for (int32_t i = i0; i < i1; i++) {
-    const int k = cls(counts[i]);
+  each_item([&](int32_t, int k) {
 #pragma unroll
     for (int x = 0; x < kOrderClasses; x++) have[x] += x == k;
-  }
+  });
 #pragma unroll
   for (int x = 0; x < kOrderClasses; x++) at[x * kOrderThreads + tid] = have[x];
   __syncthreads();
@@ -223,15 +236,14 @@ __global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(OrderLi
     start[x] = at[x * kOrderThreads];
   }
   start[kOrderClasses] = n;
-  for (int32_t i = i0; i < i1; i++) {
-    const int k = cls(counts[i]);
+  each_item([&](int32_t i, int k) {
 #pragma unroll
     for (int x = 0; x < kOrderClasses; x++)
       if (x == k) {
         order[start[x] + spread(next[x] - start[x], start[x + 1] - start[x])] = i;
         next[x]++;
       }
-  }
+  });
 }
 
 // Where this lane reads a tile of rows of D channels in LDS, in bytes from the tile's start: `rows` for the operand of
@@ -606,10 +618,14 @@ __global__ __launch_bounds__(256) void psa_mapped_rows_kernel(MapArgs a) {
   }
 }
 
+// Waves per SIMD of dq's kernel: at head dim 64 the registers allow more than two, and no unit alone bounds it (12 heads
+// x 16000, dq, dk and dv: block 64 784 us with two, 761 with three, 783 with four; block 128 761, 759, 740).
+constexpr int dq_waves(int d, int blk) { return d == 128 ? 2 : blk == 64 ? 3 : 4; }
+
 // SPLIT (here and for dk and dv): few blocks; `parts` workgroups share one, each takes a part of its list (dkv: of its
 // query heads first) and leaves its sums in the workspace, where psa_mapped_sum_kernel adds them.
 template <int D, int BLK, bool SPLIT>
-__global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_dq_kernel(MapArgs a) {
+__global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_waves(D, BLK), dq_waves(D, BLK)))) void psa_mapped_dq_kernel(MapArgs a) {
   using T = Tile<D, BLK>;
   constexpr int HK = BLK / 2, W = 2 * T::kWaves, DH = T::DT / 2;
   __shared__ __attribute__((aligned(1024))) uint8_t sk[2][T::BYTES];
