@@ -869,7 +869,8 @@ psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_
   a.row_counts = (int32_t*)((char*)workspace + l.row_counts);
   a.row_order = (int32_t*)((char*)workspace + l.row_order);
   a.col_counts = (int32_t*)((char*)workspace + l.col_counts);
-  a.col_order = (int32_t*)((char*)workspace + l.col_order);
+  a.col_order = (int2*)((char*)workspace + l.col_order);
+  a.col_split = (int4*)((char*)workspace + l.col_split) + 1;
   a.part_q = (float*)((char*)workspace + l.part_q);
   a.part_k = (float*)((char*)workspace + l.part_k);
   a.part_v = (float*)((char*)workspace + l.part_v);

@@ -38,7 +38,9 @@ struct MapArgs {
   int32_t *row_counts, *row_order;    // list lengths of the (head, query block) items and their order
   int32_t *pair_counts, *pair_order;  // forward, block 64: those of pairs of query blocks, and
   int32_t* paired;                    // whether pairs run (null: they do not)
-  int32_t *col_counts, *col_order;    // backward: those of the (key head, key block) items
+  int32_t* col_counts;                // backward: those of the (key head, key block) items, their order in pieces, and
+  int2* col_order;                    // the items that are cut (see psa_mapped_col_order_kernel)
+  int4* col_split;
   int32_t n_bh, n_heads, group;       // group: query heads per key head
   float *part_q, *part_k, *part_v;    // backward in parts: [item][parts][block][d]
   int32_t n_q, n_k, nbq, nbk, block, parts;
@@ -55,7 +57,7 @@ MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, i
 hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);
 struct MapBwdLayout {
   int32_t parts, head_parts, list_parts;
-  size_t neg_delta, row_counts, row_order, col_counts, col_order, part_q, part_k, part_v, total;  // (neg_lse2 first)
+  size_t neg_delta, row_counts, row_order, col_counts, col_order, col_split, part_q, part_k, part_v, total;  // (neg_lse2 first)
 };
 MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_bwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);

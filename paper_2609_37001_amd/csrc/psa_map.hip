@@ -101,8 +101,8 @@ __device__ __forceinline__ bool pairs_pay(unsigned long long either, unsigned lo
 __device__ __forceinline__ int2 pair_of(int32_t p, int32_t nbq) { return make_int2(2 * p, 2 * p + 1 < nbq ? 2 * p + 1 : -1); }
 
 // Kept key blocks of every (head, query block), and, if asked, those that either block of a pair keeps; a wave per pair.
-__global__ __launch_bounds__(256) void psa_mapped_row_count_kernel(MapArgs a) {
-  const int32_t item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, np = pairs_per_head(a.nbq);
+__device__ __forceinline__ void count_rows(const MapArgs& a, int32_t group) {
+  const int32_t item = group * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, np = pairs_per_head(a.nbq);
   if (item >= a.n_bh * np) return;
   const int32_t bh = item / np, b = bh / a.n_heads, hd = bh - b * a.n_heads;
   const int2 pr = pair_of(item - bh * np, a.nbq);
@@ -130,11 +130,11 @@ __global__ __launch_bounds__(256) void psa_mapped_row_count_kernel(MapArgs a) {
 }
 
 // Kept (query head, query block) pairs of every (key head, key block); 64 key blocks per workgroup.
-__global__ __launch_bounds__(256) void psa_mapped_col_count_kernel(MapArgs a) {
+__device__ __forceinline__ void count_cols(const MapArgs& a, int32_t group) {
   __shared__ int32_t part[4][64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int32_t n_kv = a.n_heads / a.group, per = (a.nbk + 63) / 64, bk = blockIdx.x / per, b = bk / n_kv, hk = bk - b * n_kv;
-  const int32_t kb = (blockIdx.x - bk * per) * 64 + lane;
+  const int32_t n_kv = a.n_heads / a.group, per = (a.nbk + 63) / 64, bk = group / per, b = bk / n_kv, hk = bk - b * n_kv;
+  const int32_t kb = (group - bk * per) * 64 + lane;
   // the rows of a key head's query heads lie one behind the other
   const uint8_t* col = a.map + b * a.map_stride_b + (int64_t)hk * a.group * a.nbq * a.nbk + min(kb, a.nbk - 1);
   int32_t c = 0;
@@ -145,64 +145,112 @@ __global__ __launch_bounds__(256) void psa_mapped_col_count_kernel(MapArgs a) {
   if (wave == 0 && kb < a.nbk) a.col_counts[bk * a.nbk + kb] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
 }
 
-constexpr int kOrderThreads = 1024, kOrderClasses = 8, kOrderRun = 8;
-
-// Sum of a list over the workgroup, in every thread.
-__device__ __forceinline__ unsigned long long list_sum(const int32_t* counts, int32_t n, unsigned long long* total) {
-  __syncthreads();
-  if (threadIdx.x == 0) *total = 0;
-  __syncthreads();
-  unsigned long long mine = 0;
-#pragma unroll 8
-  for (int32_t i = threadIdx.x; i < n; i += kOrderThreads) mine += counts[i];
-  atomicAdd(total, mine);
-  __syncthreads();
-  return *total;
+// Per query row, in blocks of `block` rows: -lse log2(e), and -delta, where the sums of dP start.  Rows behind the last
+// one, and rows that keep nothing (lse = -inf), get -inf: every weight formed with it is 0.  D / 8 lanes a row.
+template <int D>
+__device__ __forceinline__ void form_row_values(const MapArgs& a, int32_t group) {
+  constexpr int L = D / 8;
+  const int64_t r = (int64_t)group * (256 / L) + threadIdx.x / L;
+  const int32_t padded = a.nbq * a.block;
+  if (r >= (int64_t)a.n_bh * padded) return;
+  const int c = threadIdx.x % L;
+  const int32_t bh = (int32_t)(r / padded), row = (int32_t)(r - (int64_t)bh * padded);
+  const int64_t at = (int64_t)bh * a.n_q + min(row, a.n_q - 1);
+  const f32x8 x = __builtin_convertvector(*(const bf16x8*)(a.grad_o + at * D + 8 * c), f32x8);
+  const f32x8 y = __builtin_convertvector(*(const bf16x8*)(a.o + at * D + 8 * c), f32x8);
+  float s = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; e++) s = fmaf(x[e], y[e], s);
+#pragma unroll
+  for (int off = L / 2; off > 0; off >>= 1) s += __shfl_xor(s, off);
+  if (c == 0) {
+    const float lse = a.lse[at];
+    const bool none = row >= a.n_q || lse == -__builtin_inff();
+    a.neg_lse2[r] = none ? -__builtin_inff() : -lse * kLog2e;
+    a.neg_delta[r] = none ? 0.0f : -s;
+  }
 }
 
-// order[workgroup] = item: eight classes of list lengths around the mean, longest first, each in the items' order and
-// spread over the XCDs.  One workgroup per list of items; each thread takes a run of them.  Pairs' lists come second:
-// their workgroup also says whether they pay (pairs_pay).
-struct OrderList {
-  const int32_t* counts;
-  int32_t* order;
-  int32_t n;
-};
-__global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(OrderList l0, OrderList l1, int32_t* __restrict__ paired,
-                                                                         int32_t head_dim) {
-  __shared__ int32_t at[kOrderClasses * kOrderThreads];
-  __shared__ int32_t waves[kOrderThreads / 64];
-  __shared__ unsigned long long total;
-  const int32_t* counts = blockIdx.x ? l1.counts : l0.counts;
-  int32_t* order = blockIdx.x ? l1.order : l0.order;
-  const int32_t n = blockIdx.x ? l1.n : l0.n;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int32_t each = (n + kOrderThreads - 1) / kOrderThreads, i0 = min(n, tid * each), i1 = min(n, i0 + each);
-  const unsigned long long work = list_sum(counts, n, &total);
-  if (paired && blockIdx.x == 1) {
-    const unsigned long long single = list_sum(l0.counts, l0.n, &total);
-    if (tid == 0) *paired = pairs_pay(work, single, n, head_dim) ? 1 : 0;
+// What the main kernels need first, in one launch: the row values of a backward call and the list lengths.  (Three
+// launches took 8 us more.)
+template <int D>
+__global__ __launch_bounds__(256) void psa_mapped_prepare_kernel(MapArgs a, int32_t value_groups, int32_t row_groups) {
+  int32_t group = blockIdx.x;
+  if (group < value_groups) {
+    form_row_values<D>(a, group);
+  } else if ((group -= value_groups) < row_groups) {
+    count_rows(a, group);
+  } else {
+    count_cols(a, group - row_groups);
   }
-  const float mean = (float)work / (float)n;
-  auto cls = [&](int32_t c) {
-    const float x = (float)c;
-    return x >= 4.0f * mean ? 0 : x >= 2.83f * mean ? 1 : x >= 2.0f * mean ? 2 : x >= 1.5f * mean ? 3 :
-           x >= 1.25f * mean ? 4 : x >= 1.1f * mean ? 5 : x >= 0.9f * mean ? 6 : 7;
-  };
-  // A thread's items in runs of kOrderRun, whose counts are read at once (one after the other their latencies were
-  // most of the kernel: 20 us for 8896 items).
-  auto each_item = [&](auto f) {
+}
+
+constexpr int kOrderThreads = 1024, kOrderClasses = 8, kOrderRun = 8;
+
+// One workgroup of kOrderThreads over a list of items; each thread takes a run of them.
+struct Items {
+  const int32_t* counts;
+  int32_t n, i0, i1;
+  __device__ __forceinline__ Items(const int32_t* counts_, int32_t n_) : counts(counts_), n(n_) {
+    const int32_t each = (n + kOrderThreads - 1) / kOrderThreads;
+    i0 = min(n, (int32_t)threadIdx.x * each);
+    i1 = min(n, i0 + each);
+  }
+  // f(item, its count) over this thread's items, whose counts are read kOrderRun at a time (one after the other their
+  // latencies were most of the kernel: 20 us for 8896 items).
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
     for (int32_t i = i0; i < i1; i += kOrderRun) {
       int32_t c[kOrderRun];
 #pragma unroll
       for (int u = 0; u < kOrderRun; u++) c[u] = counts[min(i + u, n - 1)];
 #pragma unroll
       for (int u = 0; u < kOrderRun; u++)
-        if (i + u < i1) f(i + u, cls(c[u]));
+        if (i + u < i1) f(i + u, c[u]);
     }
-  };
+  }
+  // Sum of the counts, in every thread.
+  __device__ __forceinline__ unsigned long long sum(unsigned long long* total) const {
+    __syncthreads();
+    if (threadIdx.x == 0) *total = 0;
+    __syncthreads();
+    unsigned long long mine = 0;
+    each([&](int32_t, int32_t c) { mine += c; });
+    atomicAdd(total, mine);
+    __syncthreads();
+    return *total;
+  }
+};
+
+// Exclusive sum of a value over the workgroup's threads; *all: of every thread's.
+__device__ __forceinline__ int32_t sum_before(int32_t v, int32_t* waves, int32_t* all) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  int32_t up = v;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int32_t y = __shfl_up(up, off);
+    if (lane >= off) up += y;
+  }
+  __syncthreads();
+  if (lane == 63) waves[wave] = up;
+  __syncthreads();
+  int32_t before = up - v, sum = 0;
+  for (int w = 0; w < kOrderThreads / 64; w++) {
+    before += w < wave ? waves[w] : 0;
+    sum += waves[w];
+  }
+  *all = sum;
+  return before;
+}
+
+// Places the items that cls does not skip (-1): emit(item, place), the places from 0 on.  Eight classes of list lengths,
+// the longest first, each in the items' order and spread over the XCDs.
+template <typename K, typename E>
+__device__ __forceinline__ void place_items(const Items& items, int32_t* at, int32_t* waves, K cls, E emit) {
+  const int tid = threadIdx.x;
   int32_t have[kOrderClasses] = {};
-  each_item([&](int32_t, int k) {
+  items.each([&](int32_t, int32_t c) {
+    const int k = cls(c);
 #pragma unroll
     for (int x = 0; x < kOrderClasses; x++) have[x] += x == k;
   });
@@ -210,22 +258,13 @@ __global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(OrderLi
   for (int x = 0; x < kOrderClasses; x++) at[x * kOrderThreads + tid] = have[x];
   __syncthreads();
   // exclusive sums over (class, thread): eight entries a thread, then over the threads
-  int32_t v[kOrderClasses], sum = 0;
+  int32_t v[kOrderClasses], sum = 0, all;
 #pragma unroll
   for (int x = 0; x < kOrderClasses; x++) {
     v[x] = sum;
     sum += at[tid * kOrderClasses + x];
   }
-  int32_t up = sum;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int32_t y = __shfl_up(up, off);
-    if (lane >= off) up += y;
-  }
-  if (lane == 63) waves[wave] = up;
-  __syncthreads();
-  int32_t before = up - sum;
-  for (int w = 0; w < wave; w++) before += waves[w];
+  const int32_t before = sum_before(sum, waves, &all);
 #pragma unroll
   for (int x = 0; x < kOrderClasses; x++) at[tid * kOrderClasses + x] = before + v[x];
   __syncthreads();
@@ -235,15 +274,95 @@ __global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(OrderLi
     next[x] = at[x * kOrderThreads + tid];
     start[x] = at[x * kOrderThreads];
   }
-  start[kOrderClasses] = n;
-  each_item([&](int32_t i, int k) {
+  start[kOrderClasses] = all;
+  items.each([&](int32_t i, int32_t c) {
+    const int k = cls(c);
 #pragma unroll
     for (int x = 0; x < kOrderClasses; x++)
       if (x == k) {
-        order[start[x] + spread(next[x] - start[x], start[x + 1] - start[x])] = i;
+        emit(i, start[x] + spread(next[x] - start[x], start[x + 1] - start[x]));
         next[x]++;
       }
   });
+}
+
+__device__ __forceinline__ int length_class(int32_t c, float mean) {
+  const float x = (float)c;
+  return x >= 4.0f * mean ? 0 : x >= 2.83f * mean ? 1 : x >= 2.0f * mean ? 2 : x >= 1.5f * mean ? 3 :
+         x >= 1.25f * mean ? 4 : x >= 1.1f * mean ? 5 : x >= 0.9f * mean ? 6 : 7;
+}
+
+struct OrderSpace {
+  int32_t at[kOrderClasses * kOrderThreads], waves[kOrderThreads / 64];
+  unsigned long long total;
+};
+
+// row_order[workgroup] = (head, query block); for pairs of query blocks pair_order, and whether they pay (pairs_pay).
+__device__ __forceinline__ void order_rows(const MapArgs& a, bool pairs, int32_t head_dim, OrderSpace& s) {
+  const Items rows(a.row_counts, a.n_bh * a.nbq);
+  const Items items = pairs ? Items(a.pair_counts, a.n_bh * pairs_per_head(a.nbq)) : rows;
+  int32_t* order = pairs ? a.pair_order : a.row_order;
+  const unsigned long long work = items.sum(&s.total);
+  if (pairs) {
+    const unsigned long long single = rows.sum(&s.total);
+    if (threadIdx.x == 0) *a.paired = pairs_pay(work, single, items.n, head_dim) ? 1 : 0;
+  }
+  const float mean = (float)work / (float)items.n;
+  place_items(items, s.at, s.waves, [&](int32_t c) { return length_class(c, mean); },
+              [&](int32_t i, int32_t place) { order[place] = i; });
+}
+
+// The (key head, key block) items of dk and dv, whose lists differ the most: a block that every row keeps (text, the
+// first block of a sequence) lists the rows of every query head.  Such a list can outlast all the others together, so
+// lists longer than 1.25 of a workgroup's share of the work go in pieces of half that share (8 blocks at least), each
+// to a workgroup of its own that leaves its sums in the workspace; psa_mapped_piece_sum_kernel adds them.  (Shorter
+// ones, started first, end with the others.)  With `room` workgroups sharing the work there are at most 0.8 room such
+// lists and 2.8 room pieces, whatever the map.  Whole call, every row keeping the first block and others by chance,
+// without pieces and with them, in us: 12 heads x 32760 (D 128, blocks of 128, 8 kept) 1247 and 1031; 16 heads over 4
+// 3815 and 1298; 12 x 16384 (D 64, blocks of 64, 12 kept) 342 and 249; 32 over 8 x 16384 (D 128, blocks of 64, 16 kept)
+// 2060 and 1280.  Maps without such a block pay 0 to 2 %.
+//   col_order[workgroup] = (item, piece << 16 | pieces): the pieces first, then the whole items by their lengths,
+//                          then -1
+//   col_split[i]         = (item, workgroup of its first piece, pieces), col_split[-1].x their number
+constexpr int kPieceBlocks = 8;
+__host__ __device__ constexpr int32_t max_pieces(int32_t room) { return 3 * room; }
+__host__ __device__ constexpr int32_t max_split(int32_t room) { return room; }
+__device__ __forceinline__ void order_cols(const MapArgs& a, int32_t room, OrderSpace& s) {
+  const Items items(a.col_counts, a.n_bh / a.group * a.nbk);
+  const float work = (float)items.sum(&s.total), share = work / (float)room, mean = work / (float)items.n;
+  const float piece = fmaxf((float)kPieceBlocks, 0.5f * share), longest = fmaxf(1.5f * kPieceBlocks, 1.25f * share);
+  auto pieces_of = [&](int32_t c) { return (float)c > longest ? (int32_t)ceilf((float)c / piece) : 0; };
+  int32_t split = 0, pieces = 0, all_split, all_pieces;
+  items.each([&](int32_t, int32_t c) {
+    const int32_t p = pieces_of(c);
+    split += p > 0;
+    pieces += p;
+  });
+  split = sum_before(split, s.waves, &all_split);
+  pieces = sum_before(pieces, s.waves, &all_pieces);
+  if (threadIdx.x == 0) a.col_split[-1] = make_int4(all_split, 0, 0, 0);
+  items.each([&](int32_t i, int32_t c) {
+    const int32_t p = pieces_of(c);
+    if (p == 0) return;
+    a.col_split[split++] = make_int4(i, pieces, p, 0);
+    for (int32_t x = 0; x < p; x++) a.col_order[pieces++] = make_int2(i, x << 16 | p);
+  });
+  place_items(items, s.at, s.waves, [&](int32_t c) { return pieces_of(c) > 0 ? -1 : length_class(c, mean); },
+              [&](int32_t i, int32_t place) { a.col_order[all_pieces + place] = make_int2(i, 1); });
+  const int32_t used = all_pieces + items.n - all_split;
+  for (int32_t i = used + threadIdx.x; i < items.n + max_pieces(room); i += kOrderThreads) a.col_order[i] = make_int2(-1, 0);
+}
+
+// Up to two orders, a workgroup each.
+enum class Order { kRows, kPairs, kCols };
+__global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(MapArgs a, Order first, Order second,
+                                                                         int32_t head_dim, int32_t room) {
+  __shared__ OrderSpace space;
+  const Order which = blockIdx.x == 0 ? first : second;
+  if (which == Order::kCols)
+    order_cols(a, room, space);
+  else
+    order_rows(a, which == Order::kPairs, head_dim, space);
 }
 
 // Where this lane reads a tile of rows of D channels in LDS, in bytes from the tile's start: `rows` for the operand of
@@ -592,38 +711,12 @@ __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
 // Backward.
 // ---------------------------------------------------------------------------------------------
 
-// Per query row, in blocks of `block` rows: -lse log2(e), and -delta, where the sums of dP start.  Rows behind the last
-// one, and rows that keep nothing (lse = -inf), get -inf: every weight formed with it is 0.  D / 8 lanes a row.
-template <int D>
-__global__ __launch_bounds__(256) void psa_mapped_rows_kernel(MapArgs a) {
-  constexpr int L = D / 8;
-  const int64_t r = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-  const int32_t padded = a.nbq * a.block;
-  if (r >= (int64_t)a.n_bh * padded) return;
-  const int c = threadIdx.x % L;
-  const int32_t bh = (int32_t)(r / padded), row = (int32_t)(r - (int64_t)bh * padded);
-  const int64_t at = (int64_t)bh * a.n_q + min(row, a.n_q - 1);
-  const f32x8 x = __builtin_convertvector(*(const bf16x8*)(a.grad_o + at * D + 8 * c), f32x8);
-  const f32x8 y = __builtin_convertvector(*(const bf16x8*)(a.o + at * D + 8 * c), f32x8);
-  float s = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 8; e++) s = fmaf(x[e], y[e], s);
-#pragma unroll
-  for (int off = L / 2; off > 0; off >>= 1) s += __shfl_xor(s, off);
-  if (c == 0) {
-    const float lse = a.lse[at];
-    const bool none = row >= a.n_q || lse == -__builtin_inff();
-    a.neg_lse2[r] = none ? -__builtin_inff() : -lse * kLog2e;
-    a.neg_delta[r] = none ? 0.0f : -s;
-  }
-}
-
 // Waves per SIMD of dq's kernel: at head dim 64 the registers allow more than two, and no unit alone bounds it (12 heads
 // x 16000, dq, dk and dv: block 64 784 us with two, 761 with three, 783 with four; block 128 761, 759, 740).
 constexpr int dq_waves(int d, int blk) { return d == 128 ? 2 : blk == 64 ? 3 : 4; }
 
-// SPLIT (here and for dk and dv): few blocks; `parts` workgroups share one, each takes a part of its list (dkv: of its
-// query heads first) and leaves its sums in the workspace, where psa_mapped_sum_kernel adds them.
+// SPLIT: few query blocks; `parts` workgroups share one, each takes a part of its list and leaves its sums in the
+// workspace, where psa_mapped_sum_kernel adds them.
 template <int D, int BLK, bool SPLIT>
 __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_waves(D, BLK), dq_waves(D, BLK)))) void psa_mapped_dq_kernel(MapArgs a) {
   using T = Tile<D, BLK>;
@@ -740,7 +833,11 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_wave
   }
 }
 
-template <int D, int BLK, bool SPLIT>
+// How dk's and dv's key blocks are shared out: one workgroup each; head_parts * list_parts workgroups each, the query heads
+// first (few blocks); or as order_cols says (many).
+enum class Share { kWhole, kParts, kOrder };
+
+template <int D, int BLK, Share SHARE>
 __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_dkv_kernel(MapArgs a) {
   using T = Tile<D, BLK>;
   constexpr int HQ = BLK / 2, W = 2 * T::kWaves;
@@ -750,9 +847,20 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ int32_t found[W];
   extern __shared__ uint16_t list[];          // nbq entries
 
-  const int32_t whole = a.col_order ? a.col_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
-  const int32_t parts = SPLIT ? a.head_parts * a.list_parts : 1;
-  const int32_t item = SPLIT ? whole / parts : whole, part = SPLIT ? whole - item * parts : 0;
+  int32_t item, part = 0, parts = 1, tile = 0;             // tile: of the parts' sums
+  if constexpr (SHARE == Share::kOrder) {
+    const int2 e = a.col_order[blockIdx.x];
+    if (e.x < 0) return;
+    item = e.x;
+    part = e.y >> 16;
+    parts = e.y & 0xffff;
+    tile = blockIdx.x;
+  } else {
+    tile = item_of(blockIdx.x, gridDim.x);
+    if constexpr (SHARE == Share::kParts) parts = a.head_parts * a.list_parts;
+    item = tile / parts;
+    part = tile - item * parts;
+  }
   const int32_t bk = item / a.nbk, kb = item - bk * a.nbk, n_kv = a.n_heads / a.group;
   const int32_t b = bk / n_kv, hk = bk - b * n_kv;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
@@ -773,30 +881,48 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const Stream<D, BLK> stream(wave_s, lane);
   const LaneAt<D> at_lane(lane);
 
-  // the query heads of this workgroup, and its part of each one's list
-  const int32_t hp = SPLIT ? part / a.list_parts : 0, lp = SPLIT ? part - hp * a.list_parts : 0;
-  const int32_t hd0 = hk * a.group + (SPLIT ? a.group * hp / a.head_parts : 0);
-  const int32_t hd1 = hk * a.group + (SPLIT ? a.group * (hp + 1) / a.head_parts : a.group);
+  // the query heads of this workgroup, and its part of each one's list, or of all their lists one behind the other
+  int32_t hd0 = hk * a.group, hd1 = hd0 + a.group, lp = 0;
+  if constexpr (SHARE == Share::kParts) {
+    const int32_t hp = part / a.list_parts;
+    lp = part - hp * a.list_parts;
+    hd1 = hd0 + a.group * (hp + 1) / a.head_parts;
+    hd0 += a.group * hp / a.head_parts;
+  }
+  int32_t lo = 0, hi = 0;
+  if constexpr (SHARE == Share::kOrder) {
+    const int64_t all = a.col_counts[item];
+    lo = (int32_t)(all * part / parts);
+    hi = (int32_t)(all * (part + 1) / parts);
+  }
   for (int32_t hd = hd0; hd < hd1; hd++) {
+    if (SHARE == Share::kOrder && hi <= 0) break;
     const int64_t bh = (int64_t)b * a.n_heads + hd;
     const __bf16 *qh = a.q + bh * n_q * D, *gh = a.grad_o + bh * n_q * D;
     // This wave's 64 of the 2 BLK row values of a block (waves behind them load none).
-    const int part = wave_s * 64 / BLK, place = wave_s * 64 % BLK;
-    const float* sh = (part == 0 ? a.neg_lse2 : a.neg_delta) + bh * a.nbq * BLK + place;
+    const int which = wave_s * 64 / BLK, place = wave_s * 64 % BLK;
+    const float* sh = (which == 0 ? a.neg_lse2 : a.neg_delta) + bh * a.nbq * BLK + place;
     // (its barriers also separate the buffers from the head before)
     const uint8_t* kept = a.map + b * a.map_stride_b + (int64_t)hd * a.nbq * a.nbk + kb;
     int32_t nu = kept_list<W>(a.nbq, list, found, [&](int32_t i) { return kept[(int64_t)i * a.nbk] ? i : -1; });
     int32_t first = 0;
-    if constexpr (SPLIT) {
+    if constexpr (SHARE == Share::kParts) {
       first = (int32_t)((int64_t)nu * lp / a.list_parts);
       nu = (int32_t)((int64_t)nu * (lp + 1) / a.list_parts) - first;
+    }
+    if constexpr (SHARE == Share::kOrder) {
+      const int32_t len = nu;
+      first = max(0, min(len, lo));
+      nu = max(0, min(len, hi)) - first;
+      lo -= len;
+      hi -= len;
     }
     auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[first + i]); };
     auto issue = [&](int i) {
       const int qb = entry(i);
       stream.load(qh, lds_address(sq[i & 1]), qb, n_q);
       stream.load(gh, lds_address(sg[i & 1]), qb, n_q);
-      if (part < 2) dma4(lds_address(&stat[i & 1][part][place]), lane, sh + (int64_t)qb * BLK);
+      if (which < 2) dma4(lds_address(&stat[i & 1][which][place]), lane, sh + (int64_t)qb * BLK);
     };
     if (nu > 0) issue(0);
     for (int i = 0; i < nu; i++) {
@@ -847,8 +973,9 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
         out[(j * 4 + x) * 64][e] = grp == 0 ? dk[j][4 * x + e] : dv[j][4 * x + e];
   __syncthreads();
   const f32x4* in = slot((1 - grp) * T::kWaves + gw);
-  if (SPLIT || key < n_k) {
-    const int64_t dst = (SPLIT ? (int64_t)whole * BLK + gw * 32 + r32 : (int64_t)bk * n_k + key) * D + 4 * h;
+  const bool partial = SHARE != Share::kWhole && parts > 1;
+  if (partial || key < n_k) {
+    const int64_t dst = (partial ? (int64_t)tile * BLK + gw * 32 + r32 : (int64_t)bk * n_k + key) * D + 4 * h;
 #pragma unroll
     for (int j = 0; j < T::DT; j++) {
       f32x16 t;
@@ -857,7 +984,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int e = 0; e < 4; e++)
           t[4 * x + e] = (grp == 0 ? dv[j][4 * x + e] : dk[j][4 * x + e]) + in[(j * 4 + x) * 64][e];
-      if constexpr (SPLIT)
+      if (partial)
         store_cols((grp == 0 ? a.part_v : a.part_k) + dst + 32 * j, t);
       else
         store_cols((grp == 0 ? a.dv : a.dk) + dst + 32 * j, t, grp == 0 ? 1.0f : a.scale);
@@ -886,6 +1013,28 @@ __global__ __launch_bounds__(256) void psa_mapped_sum_kernel(PartSums p) {
   *(bf16x4*)(p.out[which] + r * D + 4 * c) = __builtin_convertvector(s * p.scale[which], bf16x4);
 }
 
+// dk and dv of the key blocks that went in pieces, four 16-byte columns a thread.
+template <int D, int BLK>
+__global__ __launch_bounds__(256) void psa_mapped_piece_sum_kernel(MapArgs a) {
+  constexpr int L = D / 4;
+  if ((int32_t)blockIdx.x >= a.col_split[-1].x) return;
+  const int4 e = a.col_split[blockIdx.x];
+  const bool values = blockIdx.y & 1;
+  const int32_t bk = e.x / a.nbk, key0 = (e.x - bk * a.nbk) * BLK;
+  const f32x4* src = (const f32x4*)(values ? a.part_v : a.part_k) + (int64_t)e.y * (BLK * L);
+  __bf16* dst = (values ? a.dv : a.dk) + ((int64_t)bk * a.n_k + key0) * D;
+  f32x4 s[4] = {};
+  const int at = (blockIdx.y >> 1) * 1024 + threadIdx.x;
+#pragma unroll 2
+  for (int i = 0; i < e.z; i++)
+#pragma unroll
+    for (int u = 0; u < 4; u++) s[u] += src[(int64_t)i * (BLK * L) + at + 256 * u];
+#pragma unroll
+  for (int u = 0; u < 4; u++)
+    if (key0 + (at + 256 * u) / L < a.n_k)
+      *(bf16x4*)(dst + 4 * (at + 256 * u)) = __builtin_convertvector(s[u] * (values ? 1.0f : a.scale), bf16x4);
+}
+
 template <int D, int BLK>
 hipError_t launch_sums(const PartSums& p, int tensors, hipStream_t stream) {
   const int64_t rows = (int64_t)p.heads * p.n;
@@ -895,7 +1044,8 @@ hipError_t launch_sums(const PartSums& p, int tensors, hipStream_t stream) {
 }
 
 // Whether the items are more than the workgroups that run at once (one of 128 rows to a CU, two of 64).
-bool ordered(int64_t items, int32_t block) { return items > 256 * (128 / block); }
+int32_t room_of(int32_t block) { return 256 * (128 / block); }
+bool ordered(int64_t items, int32_t block) { return items > room_of(block); }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -915,7 +1065,7 @@ hipError_t by_shape(int32_t head_dim, int32_t block, F f) {
 // (two of 64 rows to a CU, one of 128), each part at least six blocks of a full row: the parts' sums cost a kernel more, 4 us,
 // and a block 0.5 to 1.3 us.
 int32_t map_parts(int32_t n_bh, int32_t nbq, int32_t nbk, int32_t block) {
-  const int64_t items = (int64_t)n_bh * nbq, room = 256 * (128 / block);
+  const int64_t items = (int64_t)n_bh * nbq, room = room_of(block);
   return (int32_t)std::max<int64_t>(1, std::min<int64_t>(room / items, nbk / 6));
 }
 
@@ -940,53 +1090,58 @@ MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, i
 MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
   const size_t rows = up256((size_t)n_bh * nbq * block * sizeof(float));
   const size_t q_items = up256((size_t)n_bh * nbq * sizeof(int32_t)), k_items = up256((size_t)n_kv * nbk * sizeof(int32_t));
+  const bool by_col = ordered((int64_t)n_kv * nbk, block);
+  const int32_t pieces = max_pieces(room_of(block));
   const size_t tile = (size_t)block * head_dim * sizeof(float);
   MapBwdLayout l;
   // dq's lists are shared out as the forward's; dk's and dv's over the query heads of a key head first
   l.parts = map_parts(n_bh, nbq, nbk, block);
-  const int32_t group = n_bh / n_kv, room = std::max(1, (int32_t)(256 * (128 / block) / ((int64_t)n_kv * nbk)));
+  const int32_t group = n_bh / n_kv, room = std::max(1, (int32_t)(room_of(block) / ((int64_t)n_kv * nbk)));
   l.head_parts = std::min(group, room);
   l.list_parts = std::max(1, std::min(room / l.head_parts, nbq / 6));
   const int32_t kv_parts = l.head_parts * l.list_parts;
   const size_t part_q = l.parts > 1 ? up256(tile * n_bh * nbq * l.parts) : 0;
-  const size_t part_kv = kv_parts > 1 ? up256(tile * n_kv * nbk * kv_parts) : 0;
+  const size_t part_kv = by_col ? up256(tile * pieces) : kv_parts > 1 ? up256(tile * n_kv * nbk * kv_parts) : 0;
   l.neg_delta = rows;
   l.row_counts = l.neg_delta + rows;
   l.row_order = l.row_counts + q_items;
   l.col_counts = l.row_order + q_items;
   l.col_order = l.col_counts + k_items;
-  l.part_q = l.col_order + k_items;
+  l.col_split = l.col_order + (by_col ? up256(((size_t)n_kv * nbk + pieces) * sizeof(int2)) : 0);
+  l.part_q = l.col_split + (by_col ? up256((1 + max_split(room_of(block))) * sizeof(int4)) : 0);
   l.part_k = l.part_q + part_q;
   l.part_v = l.part_k + part_kv;
   l.total = l.part_v + part_kv;
   return l;
 }
 
-// The orders of the rows and columns that outnumber the workgroups; clears the pointers of the others.
-static hipError_t launch_orders(MapArgs& a, int32_t head_dim, bool cols, hipStream_t stream) {
-  const int32_t n0 = a.n_bh * a.nbq, n1 = a.n_bh / a.group * a.nbk;
-  const bool by_row = ordered(n0, a.block), by_col = cols && ordered(n1, a.block);
+// What comes before the main kernels: a backward call's row values, and the orders of the rows and columns that outnumber
+// the workgroups (the pointers of the others are cleared).
+static hipError_t launch_prepare(MapArgs& a, int32_t head_dim, bool backward, hipStream_t stream) {
+  const int32_t n_kv = a.n_bh / a.group;
+  const bool by_row = ordered((int64_t)a.n_bh * a.nbq, a.block), by_col = backward && ordered((int64_t)n_kv * a.nbk, a.block);
   if (!by_row) a.row_order = nullptr;
   if (!by_col) a.col_order = nullptr;
-  if (!by_row || cols || a.block != 64) a.paired = a.pair_counts = nullptr;
-  if (!by_row && !by_col) return hipSuccess;
-  const int32_t pairs = a.n_bh * pairs_per_head(a.nbq);
-  if (by_row) hipLaunchKernelGGL(psa_mapped_row_count_kernel, dim3((pairs + 3) / 4), dim3(256), 0, stream, a);
-  if (by_col)
-    hipLaunchKernelGGL(psa_mapped_col_count_kernel, dim3((a.nbk + 63) / 64 * (a.n_bh / a.group)), dim3(256), 0, stream, a);
+  if (!by_row || backward || a.block != 64) a.paired = a.pair_counts = nullptr;
+  const int64_t value_groups = backward ? ((int64_t)a.n_bh * a.nbq * a.block * (head_dim / 8) + 255) / 256 : 0;
+  const int32_t row_groups = by_row ? (a.n_bh * pairs_per_head(a.nbq) + 3) / 4 : 0;
+  const int64_t col_groups = by_col ? (int64_t)(a.nbk + 63) / 64 * n_kv : 0;
+  const int64_t groups = value_groups + row_groups + col_groups;
+  if (groups == 0) return hipSuccess;
+  auto kernel = head_dim == 128 ? psa_mapped_prepare_kernel<128> : psa_mapped_prepare_kernel<64>;
+  hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(256), 0, stream, a, (int32_t)value_groups, row_groups);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const OrderList rows = {a.row_counts, a.row_order, n0}, col = {a.col_counts, a.col_order, n1};
-  const OrderList pair = {a.pair_counts, a.pair_order, pairs};
-  hipLaunchKernelGGL(psa_mapped_order_kernel, dim3(by_row + (by_col || a.paired)), dim3(kOrderThreads), 0, stream,
-                     by_row ? rows : col, a.paired ? pair : col, a.paired, head_dim);
+  if (e != hipSuccess || (!by_row && !by_col)) return e;
+  hipLaunchKernelGGL(psa_mapped_order_kernel, dim3(by_row && (by_col || a.paired) ? 2 : 1), dim3(kOrderThreads), 0, stream, a,
+                     by_row ? Order::kRows : Order::kCols, by_col ? Order::kCols : Order::kPairs, head_dim,
+                     room_of(a.block));
   return hipGetLastError();
 }
 
 hipError_t launch_map_fwd(const MapArgs& args, int32_t head_dim, hipStream_t stream) {
   MapArgs a = args;
   if (a.parts > 1) a.row_order = a.paired = nullptr;
-  const hipError_t e = a.parts == 1 ? launch_orders(a, head_dim, false, stream) : hipSuccess;
+  const hipError_t e = a.parts == 1 ? launch_prepare(a, head_dim, false, stream) : hipSuccess;
   if (e != hipSuccess) return e;
   return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
     constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
@@ -1015,21 +1170,28 @@ hipError_t launch_map_fwd(const MapArgs& args, int32_t head_dim, hipStream_t str
 
 hipError_t launch_map_bwd(const MapArgs& args, int32_t head_dim, hipStream_t stream) {
   MapArgs a = args;
-  hipError_t e = launch_orders(a, head_dim, true, stream);
+  hipError_t e = launch_prepare(a, head_dim, true, stream);
   if (e != hipSuccess) return e;
   return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
     constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
-    const int64_t rows = (int64_t)a.n_bh * a.nbq * B;
-    hipLaunchKernelGGL(psa_mapped_rows_kernel<D>, dim3((uint32_t)((rows * (D / 8) + 255) / 256)), dim3(256), 0, stream, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    hipError_t e = hipSuccess;
     const int32_t n_kv = a.n_bh / a.group, kv_parts = a.head_parts * a.list_parts;
-    if (kv_parts == 1) {
-      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, false>), dim3(n_kv * a.nbk), dim3(4 * B), list_bytes(a.nbq), stream, a);
+    if (a.col_order) {
+      const int32_t room = room_of(B);
+      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, Share::kOrder>), dim3(n_kv * a.nbk + max_pieces(room)), dim3(4 * B),
+                         list_bytes(a.nbq), stream, a);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((psa_mapped_piece_sum_kernel<D, B>), dim3(max_split(room), 2 * (B * D / 4096)), dim3(256), 0, stream,
+                         a);
+      e = hipGetLastError();
+    } else if (kv_parts == 1) {
+      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, Share::kWhole>), dim3(n_kv * a.nbk), dim3(4 * B), list_bytes(a.nbq),
+                         stream, a);
       e = hipGetLastError();
     } else {
-      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, true>), dim3(n_kv * a.nbk * kv_parts), dim3(4 * B), list_bytes(a.nbq),
-                         stream, a);
+      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, Share::kParts>), dim3(n_kv * a.nbk * kv_parts), dim3(4 * B),
+                         list_bytes(a.nbq), stream, a);
       e = hipGetLastError();
       if (e == hipSuccess)
         e = launch_sums<D, B>({{a.part_k, a.part_v}, {a.dk, a.dv}, {a.scale, 1.0f}, n_kv, a.n_k, a.nbk, kv_parts}, 2, stream);

@@ -172,6 +172,15 @@ def test_shared_key_heads(d, block, h, hk):
 
 
 @pytest.mark.parametrize("d,block", SHAPES)
+@pytest.mark.parametrize("h,hk,nq,density", [(104, 26, 7, 0.1), (26, 26, 61, 0.2)])
+def test_key_blocks_that_every_row_keeps(d, block, h, hk, nq, density):
+    """Many key blocks, the first and the last of them on every row's list: dk and dv in pieces."""
+    m = random_map(41, 1, h, nq, 20, density)
+    m[:, :, :nq - 2, 0] = 1
+    check(1, h, hk, nq * block - 5, 20 * block - 31, block, d, m=m, heads=[0, h - 1])
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
 @pytest.mark.parametrize("density", [0.0, 1.0])
 def test_empty_and_full_maps(d, block, density):
     nq, nk = 4, 6
