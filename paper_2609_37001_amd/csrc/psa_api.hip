@@ -824,13 +824,19 @@ psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, i
   s = check_map_workspace(workspace, workspace_bytes, l.total);
   if (s != PSA_OK) return s;
   a.parts = l.parts;
-  a.part_o = (float*)workspace;
-  a.part_ml = (float2*)((char*)workspace + l.part_ml);
-  a.row_counts = (int32_t*)workspace;
-  a.row_order = (int32_t*)((char*)workspace + l.row_order);
-  a.pair_counts = (int32_t*)((char*)workspace + l.pair_counts);
-  a.pair_order = (int32_t*)((char*)workspace + l.pair_order);
-  a.paired = (int32_t*)((char*)workspace + l.paired);
+  char* ws = (char*)workspace;
+  if (l.parts > 1) {
+    a.part_o = (float*)ws;
+    a.part_ml = (float2*)(ws + l.part_ml);
+  } else if (l.total) {
+    a.row_counts = (int32_t*)ws;
+    a.row_order = (int32_t*)(ws + l.row_order);
+    if (block == 64) {
+      a.pair_counts = (int32_t*)(ws + l.pair_counts);
+      a.pair_order = (int32_t*)(ws + l.pair_order);
+      a.paired = (int32_t*)(ws + l.paired);
+    }
+  }
   const hipError_t e = psa::launch_map_fwd(a, head_dim, stream);
   return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_attention_map_fwd launch");
 }
@@ -864,16 +870,24 @@ psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_
   a.dq = (__bf16*)dq;
   a.dk = (__bf16*)dk;
   a.dv = (__bf16*)dv;
-  a.neg_lse2 = (float*)workspace;
-  a.neg_delta = (float*)((char*)workspace + l.neg_delta);
-  a.row_counts = (int32_t*)((char*)workspace + l.row_counts);
-  a.row_order = (int32_t*)((char*)workspace + l.row_order);
-  a.col_counts = (int32_t*)((char*)workspace + l.col_counts);
-  a.col_order = (int2*)((char*)workspace + l.col_order);
-  a.col_split = (int4*)((char*)workspace + l.col_split) + 1;
-  a.part_q = (float*)((char*)workspace + l.part_q);
-  a.part_k = (float*)((char*)workspace + l.part_k);
-  a.part_v = (float*)((char*)workspace + l.part_v);
+  char* ws = (char*)workspace;
+  a.neg_lse2 = (float*)(ws + l.neg_lse2);
+  a.neg_delta = (float*)(ws + l.neg_delta);
+  a.row_pieces = l.rows;
+  if (l.rows.grid) {
+    a.row_counts = (int32_t*)(ws + l.row_counts);
+    a.row_pieces.order = (int2*)(ws + l.row_order);
+    a.row_pieces.split = (int4*)(ws + l.row_split) + 1;
+  }
+  a.col_pieces = l.cols;
+  if (l.cols.grid) {
+    a.col_counts = (int32_t*)(ws + l.col_counts);
+    a.col_pieces.order = (int2*)(ws + l.col_order);
+    a.col_pieces.split = (int4*)(ws + l.col_split) + 1;
+  }
+  a.part_q = (float*)(ws + l.part_q);
+  a.part_k = (float*)(ws + l.part_k);
+  a.part_v = (float*)(ws + l.part_v);
   a.parts = l.parts;
   a.head_parts = l.head_parts;
   a.list_parts = l.list_parts;

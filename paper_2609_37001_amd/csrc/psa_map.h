@@ -24,6 +24,13 @@ SelectLayout select_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t
 hipError_t launch_select(const SelectArgs& args, int32_t head_dim, hipStream_t stream);
 
 // Attention over a block map.
+// Order of a backward kernel's items (psa_map.hip, order_pieces): `grid` workgroups (0: there is none), of which at most
+// `pieces` take a piece of a list, of at most `splits` items.
+struct Pieces {
+  int2* order;
+  int4* split;
+  int32_t grid, pieces, splits;
+};
 struct MapArgs {
   const __bf16 *q, *k, *v;            // q [n_bh][n_q][d]; k and v by strides, rows contiguous
   const __bf16* grad_o;               // backward
@@ -35,14 +42,13 @@ struct MapArgs {
   float* part_o;                      // forward in parts: [n_bh][nbq][parts][block][d] and (m, l) of the rows
   float2* part_ml;
   float *neg_lse2, *neg_delta;        // backward: [n_bh][nbq][block]
-  int32_t *row_counts, *row_order;    // list lengths of the (head, query block) items and their order
+  int32_t *row_counts, *row_order;    // list lengths of the (head, query block) items (null: not ordered), their order
   int32_t *pair_counts, *pair_order;  // forward, block 64: those of pairs of query blocks, and
   int32_t* paired;                    // whether pairs run (null: they do not)
-  int32_t* col_counts;                // backward: those of the (key head, key block) items, their order in pieces, and
-  int2* col_order;                    // the items that are cut (see psa_mapped_col_order_kernel)
-  int4* col_split;
+  int32_t* col_counts;                // backward: those of the (key head, key block) items
+  Pieces row_pieces, col_pieces;      // backward
   int32_t n_bh, n_heads, group;       // group: query heads per key head
-  float *part_q, *part_k, *part_v;    // backward in parts: [item][parts][block][d]
+  float *part_q, *part_k, *part_v;    // backward: sums of a part of a list, [tile][block][d]
   int32_t n_q, n_k, nbq, nbk, block, parts;
   int32_t head_parts, list_parts;     // backward: parts of a key block's query heads, and of each one's list
   float c, scale;                     // scale log2(e), scale
@@ -56,8 +62,9 @@ struct MapLayout {
 MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);
 struct MapBwdLayout {
+  Pieces rows, cols;                  // sizes alone
   int32_t parts, head_parts, list_parts;
-  size_t neg_delta, row_counts, row_order, col_counts, col_order, col_split, part_q, part_k, part_v, total;  // (neg_lse2 first)
+  size_t neg_lse2, neg_delta, row_counts, row_order, row_split, col_counts, col_order, col_split, part_q, part_k, part_v, total;
 };
 MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_bwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);

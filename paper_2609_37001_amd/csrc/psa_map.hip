@@ -187,38 +187,54 @@ __global__ __launch_bounds__(256) void psa_mapped_prepare_kernel(MapArgs a, int3
 
 constexpr int kOrderThreads = 1024, kOrderClasses = 8, kOrderRun = 8;
 
-// One workgroup of kOrderThreads over a list of items; each thread takes a run of them.
+constexpr int kOrderWaves = kOrderThreads / 64;
+
+struct OrderSpace {
+  int32_t at[kOrderClasses * kOrderThreads * 33 / 32], waves[kOrderWaves];
+  unsigned long long totals[kOrderWaves];
+};
+
+// One workgroup of kOrderThreads over a list of items; each thread takes a run of them, whose first kOrderRun counts it keeps
+// (read again by every pass, their latencies were most of the kernel).
 struct Items {
   const int32_t* counts;
-  int32_t n, i0, i1;
+  int32_t n, i0, i1, kept[kOrderRun];
   __device__ __forceinline__ Items(const int32_t* counts_, int32_t n_) : counts(counts_), n(n_) {
     const int32_t each = (n + kOrderThreads - 1) / kOrderThreads;
     i0 = min(n, (int32_t)threadIdx.x * each);
     i1 = min(n, i0 + each);
+    read(kept, i0);
   }
-  // f(item, its count) over this thread's items, whose counts are read kOrderRun at a time (one after the other their
-  // latencies were most of the kernel: 20 us for 8896 items).
+  __device__ __forceinline__ void read(int32_t (&c)[kOrderRun], int32_t i) const {
+#pragma unroll
+    for (int u = 0; u < kOrderRun; u++) c[u] = counts[min(i + u, n - 1)];
+  }
+  // f(item, its count) over this thread's items.
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    for (int32_t i = i0; i < i1; i += kOrderRun) {
-      int32_t c[kOrderRun];
+    int32_t c[kOrderRun];
 #pragma unroll
-      for (int u = 0; u < kOrderRun; u++) c[u] = counts[min(i + u, n - 1)];
+    for (int u = 0; u < kOrderRun; u++) c[u] = kept[u];
+    for (int32_t i = i0; i < i1;) {
 #pragma unroll
       for (int u = 0; u < kOrderRun; u++)
         if (i + u < i1) f(i + u, c[u]);
+      i += kOrderRun;
+      if (i < i1) read(c, i);
     }
   }
   // Sum of the counts, in every thread.
-  __device__ __forceinline__ unsigned long long sum(unsigned long long* total) const {
-    __syncthreads();
-    if (threadIdx.x == 0) *total = 0;
-    __syncthreads();
-    unsigned long long mine = 0;
+  __device__ __forceinline__ unsigned long long sum(unsigned long long* totals) const {
+    unsigned long long mine = 0, all = 0;
     each([&](int32_t, int32_t c) { mine += c; });
-    atomicAdd(total, mine);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) mine += __shfl_xor(mine, off);
     __syncthreads();
-    return *total;
+    if ((threadIdx.x & 63) == 0) totals[threadIdx.x >> 6] = mine;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kOrderWaves; w++) all += totals[w];
+    return all;
   }
 };
 
@@ -235,7 +251,7 @@ __device__ __forceinline__ int32_t sum_before(int32_t v, int32_t* waves, int32_t
   if (lane == 63) waves[wave] = up;
   __syncthreads();
   int32_t before = up - v, sum = 0;
-  for (int w = 0; w < kOrderThreads / 64; w++) {
+  for (int w = 0; w < kOrderWaves; w++) {
     before += w < wave ? waves[w] : 0;
     sum += waves[w];
   }
@@ -248,6 +264,7 @@ __device__ __forceinline__ int32_t sum_before(int32_t v, int32_t* waves, int32_t
 template <typename K, typename E>
 __device__ __forceinline__ void place_items(const Items& items, int32_t* at, int32_t* waves, K cls, E emit) {
   const int tid = threadIdx.x;
+  auto cell = [&](int p) -> int32_t& { return at[p + (p >> 5)]; };       // (a lane's eight lie in banks of their own)
   int32_t have[kOrderClasses] = {};
   items.each([&](int32_t, int32_t c) {
     const int k = cls(c);
@@ -255,34 +272,38 @@ __device__ __forceinline__ void place_items(const Items& items, int32_t* at, int
     for (int x = 0; x < kOrderClasses; x++) have[x] += x == k;
   });
 #pragma unroll
-  for (int x = 0; x < kOrderClasses; x++) at[x * kOrderThreads + tid] = have[x];
+  for (int x = 0; x < kOrderClasses; x++) cell(x * kOrderThreads + tid) = have[x];
   __syncthreads();
   // exclusive sums over (class, thread): eight entries a thread, then over the threads
   int32_t v[kOrderClasses], sum = 0, all;
 #pragma unroll
   for (int x = 0; x < kOrderClasses; x++) {
     v[x] = sum;
-    sum += at[tid * kOrderClasses + x];
+    sum += cell(tid * kOrderClasses + x);
   }
   const int32_t before = sum_before(sum, waves, &all);
 #pragma unroll
-  for (int x = 0; x < kOrderClasses; x++) at[tid * kOrderClasses + x] = before + v[x];
+  for (int x = 0; x < kOrderClasses; x++) cell(tid * kOrderClasses + x) = before + v[x];
   __syncthreads();
   int32_t next[kOrderClasses], start[kOrderClasses + 1];
 #pragma unroll
   for (int x = 0; x < kOrderClasses; x++) {
-    next[x] = at[x * kOrderThreads + tid];
-    start[x] = at[x * kOrderThreads];
+    next[x] = cell(x * kOrderThreads + tid);
+    start[x] = cell(x * kOrderThreads);
   }
   start[kOrderClasses] = all;
   items.each([&](int32_t i, int32_t c) {
     const int k = cls(c);
+    if (k < 0) return;
+    int32_t first = 0, place = 0, size = 0;       // of the class (emitting within the loop would emit eight times)
 #pragma unroll
-    for (int x = 0; x < kOrderClasses; x++)
-      if (x == k) {
-        emit(i, start[x] + spread(next[x] - start[x], start[x + 1] - start[x]));
-        next[x]++;
-      }
+    for (int x = 0; x < kOrderClasses; x++) {
+      first = x == k ? start[x] : first;
+      place = x == k ? next[x] - start[x] : place;
+      size = x == k ? start[x + 1] - start[x] : size;
+      next[x] += x == k;
+    }
+    emit(i, first + spread(place, size));
   });
 }
 
@@ -292,19 +313,14 @@ __device__ __forceinline__ int length_class(int32_t c, float mean) {
          x >= 1.25f * mean ? 4 : x >= 1.1f * mean ? 5 : x >= 0.9f * mean ? 6 : 7;
 }
 
-struct OrderSpace {
-  int32_t at[kOrderClasses * kOrderThreads], waves[kOrderThreads / 64];
-  unsigned long long total;
-};
-
 // row_order[workgroup] = (head, query block); for pairs of query blocks pair_order, and whether they pay (pairs_pay).
 __device__ __forceinline__ void order_rows(const MapArgs& a, bool pairs, int32_t head_dim, OrderSpace& s) {
   const Items rows(a.row_counts, a.n_bh * a.nbq);
   const Items items = pairs ? Items(a.pair_counts, a.n_bh * pairs_per_head(a.nbq)) : rows;
   int32_t* order = pairs ? a.pair_order : a.row_order;
-  const unsigned long long work = items.sum(&s.total);
+  const unsigned long long work = items.sum(s.totals);
   if (pairs) {
-    const unsigned long long single = rows.sum(&s.total);
+    const unsigned long long single = rows.sum(s.totals);
     if (threadIdx.x == 0) *a.paired = pairs_pay(work, single, items.n, head_dim) ? 1 : 0;
   }
   const float mean = (float)work / (float)items.n;
@@ -312,26 +328,29 @@ __device__ __forceinline__ void order_rows(const MapArgs& a, bool pairs, int32_t
               [&](int32_t i, int32_t place) { order[place] = i; });
 }
 
-// The (key head, key block) items of dk and dv, whose lists differ the most: a block that every row keeps (text, the
-// first block of a sequence) lists the rows of every query head.  Such a list can outlast all the others together, so
-// lists longer than 1.25 of a workgroup's share of the work go in pieces of half that share (8 blocks at least), each
-// to a workgroup of its own that leaves its sums in the workspace; psa_mapped_piece_sum_kernel adds them.  (Shorter
-// ones, started first, end with the others.)  With `room` workgroups sharing the work there are at most 0.8 room such
-// lists and 2.8 room pieces, whatever the map.  Whole call, every row keeping the first block and others by chance,
-// without pieces and with them, in us: 12 heads x 32760 (D 128, blocks of 128, 8 kept) 1247 and 1031; 16 heads over 4
-// 3815 and 1298; 12 x 16384 (D 64, blocks of 64, 12 kept) 342 and 249; 32 over 8 x 16384 (D 128, blocks of 64, 16 kept)
-// 2060 and 1280.  Maps without such a block pay 0 to 2 %.
-//   col_order[workgroup] = (item, piece << 16 | pieces): the pieces first, then the whole items by their lengths,
-//                          then -1
-//   col_split[i]         = (item, workgroup of its first piece, pieces), col_split[-1].x their number
-constexpr int kPieceBlocks = 8;
-__host__ __device__ constexpr int32_t max_pieces(int32_t room) { return 3 * room; }
-__host__ __device__ constexpr int32_t max_split(int32_t room) { return room; }
-__device__ __forceinline__ void order_cols(const MapArgs& a, int32_t room, OrderSpace& s) {
-  const Items items(a.col_counts, a.n_bh / a.group * a.nbk);
-  const float work = (float)items.sum(&s.total), share = work / (float)room, mean = work / (float)items.n;
-  const float piece = fmaxf((float)kPieceBlocks, 0.5f * share), longest = fmaxf(1.5f * kPieceBlocks, 1.25f * share);
-  auto pieces_of = [&](int32_t c) { return (float)c > longest ? (int32_t)ceilf((float)c / piece) : 0; };
+// The lists of the backward kernels: of a (key head, key block) item for dk and dv, of a (head, query block) item for
+// dq.  Their lengths differ: a block that every row keeps (text, the first block of a sequence) lists the rows of every
+// query head, a row of text lists every key block, and such a list can outlast all the others together.  So long ones go
+// in pieces, each to a workgroup of its own that leaves its sums in the workspace; psa_mapped_sum_kernel adds them.
+// With `room` workgroups sharing the work (`share` blocks each):
+//   * more items than room: lists longer than 1.25 share, in pieces of half a share, 8 blocks at least (shorter ones,
+//     started first, end with the others).  At most 0.8 room lists and 2.8 room pieces, whatever the map.
+//   * fewer: a list of average length goes in room / items pieces and a longer one in pieces as long, 4 blocks at
+//     least.  At most 4/3 room pieces.
+// Whole calls without and with pieces, in us.  Every row keeps the first block and others by chance: 12 heads x 32760
+// (D 128, blocks of 128, 8 kept) 1247 and 1031; 16 heads over 4 3815 and 1298; 12 x 16384 (D 64, blocks of 64, 12 kept)
+// 342 and 249; 32 over 8 x 16384 (D 128, blocks of 64, 16 kept) 2060 and 1280.  Rows of text (226 tokens): 8 heads x
+// 4096 (D 128, blocks of 64, 8 kept) 181 and 124.  Maps without any of these pay 0 to 2 %.
+//   order[workgroup] = (item, piece << 16 | pieces): the pieces first, then the whole items by their lengths, then -1
+//   split[i]         = (item, workgroup of its first piece, pieces), split[-1].x their number
+constexpr int kPieceBlocks = 8, kFewBlocks = 4;
+__device__ __forceinline__ void order_pieces(const Items& items, const Pieces& to, int32_t room, OrderSpace& s) {
+  const float work = (float)items.sum(s.totals), share = work / (float)room, mean = work / (float)items.n;
+  const bool few = items.n <= room;
+  const float piece = few ? fmaxf((float)kFewBlocks, mean / (float)(room / items.n)) : fmaxf((float)kPieceBlocks, 0.5f * share);
+  const float longest = few ? 1.5f * piece : fmaxf(1.5f * kPieceBlocks, 1.25f * share);
+  const float up = few ? 0.5f : 1.0f;
+  auto pieces_of = [&](int32_t c) { return (float)c > longest ? (int32_t)((float)c / piece + up) : 0; };
   int32_t split = 0, pieces = 0, all_split, all_pieces;
   items.each([&](int32_t, int32_t c) {
     const int32_t p = pieces_of(c);
@@ -340,27 +359,30 @@ __device__ __forceinline__ void order_cols(const MapArgs& a, int32_t room, Order
   });
   split = sum_before(split, s.waves, &all_split);
   pieces = sum_before(pieces, s.waves, &all_pieces);
-  if (threadIdx.x == 0) a.col_split[-1] = make_int4(all_split, 0, 0, 0);
+  if (threadIdx.x == 0) to.split[-1] = make_int4(all_split, 0, 0, 0);
   items.each([&](int32_t i, int32_t c) {
     const int32_t p = pieces_of(c);
     if (p == 0) return;
-    a.col_split[split++] = make_int4(i, pieces, p, 0);
-    for (int32_t x = 0; x < p; x++) a.col_order[pieces++] = make_int2(i, x << 16 | p);
+    to.split[split++] = make_int4(i, pieces, p, 0);
+    for (int32_t x = 0; x < p; x++) to.order[pieces++] = make_int2(i, x << 16 | p);
   });
   place_items(items, s.at, s.waves, [&](int32_t c) { return pieces_of(c) > 0 ? -1 : length_class(c, mean); },
-              [&](int32_t i, int32_t place) { a.col_order[all_pieces + place] = make_int2(i, 1); });
-  const int32_t used = all_pieces + items.n - all_split;
-  for (int32_t i = used + threadIdx.x; i < items.n + max_pieces(room); i += kOrderThreads) a.col_order[i] = make_int2(-1, 0);
+              [&](int32_t i, int32_t place) { to.order[all_pieces + place] = make_int2(i, 1); });
+  for (int32_t i = all_pieces + items.n - all_split + threadIdx.x; i < to.grid; i += kOrderThreads)
+    to.order[i] = make_int2(-1, 0);
 }
 
-// Up to two orders, a workgroup each.
-enum class Order { kRows, kPairs, kCols };
+// Up to two orders, a workgroup each: the rows' and the pairs' of a forward call, the rows' and the columns' pieces of
+// a backward call.
+enum class Order { kRows, kPairs, kRowPieces, kColPieces };
 __global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(MapArgs a, Order first, Order second,
                                                                          int32_t head_dim, int32_t room) {
   __shared__ OrderSpace space;
   const Order which = blockIdx.x == 0 ? first : second;
-  if (which == Order::kCols)
-    order_cols(a, room, space);
+  if (which == Order::kRowPieces)
+    order_pieces(Items(a.row_counts, a.n_bh * a.nbq), a.row_pieces, room, space);
+  else if (which == Order::kColPieces)
+    order_pieces(Items(a.col_counts, a.n_bh / a.group * a.nbk), a.col_pieces, room, space);
   else
     order_rows(a, which == Order::kPairs, head_dim, space);
 }
@@ -715,9 +737,39 @@ __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
 // x 16000, dq, dk and dv: block 64 784 us with two, 761 with three, 783 with four; block 128 761, 759, 740).
 constexpr int dq_waves(int d, int blk) { return d == 128 ? 2 : blk == 64 ? 3 : 4; }
 
-// SPLIT: few query blocks; `parts` workgroups share one, each takes a part of its list and leaves its sums in the
-// workspace, where psa_mapped_sum_kernel adds them.
-template <int D, int BLK, bool SPLIT>
+// How the lists of a backward kernel are shared out: a workgroup each; the same number of parts each; or as order_pieces
+// says.
+enum class Share { kWhole, kParts, kOrder };
+
+// A workgroup's item and its part of the item's list, whose sums go to `tile` of the workspace if there are several.
+template <Share SHARE>
+struct Piece {
+  int32_t item, part = 0, parts = 1, tile;
+  __device__ __forceinline__ Piece(const Pieces& order, int32_t equal_parts) {
+    if constexpr (SHARE == Share::kOrder) {
+      tile = blockIdx.x;
+      const int2 e = order.order[tile];
+      item = e.x;
+      part = e.y >> 16;
+      parts = e.y & 0xffff;
+    } else {
+      item = tile = item_of(blockIdx.x, gridDim.x);
+      if constexpr (SHARE == Share::kParts) {
+        parts = equal_parts;
+        item = tile / parts;
+        part = tile - item * parts;
+      }
+    }
+  }
+  __device__ __forceinline__ bool none() const { return SHARE == Share::kOrder && item < 0; }
+  __device__ __forceinline__ bool partial() const { return SHARE != Share::kWhole && parts > 1; }
+};
+// Where a part of a list of n starts.
+__device__ __forceinline__ int32_t part_start(int32_t n, int32_t part, int32_t parts) {
+  return (int32_t)((int64_t)n * part / parts);
+}
+
+template <int D, int BLK, Share SHARE>
 __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_waves(D, BLK), dq_waves(D, BLK)))) void psa_mapped_dq_kernel(MapArgs a) {
   using T = Tile<D, BLK>;
   constexpr int HK = BLK / 2, W = 2 * T::kWaves, DH = T::DT / 2;
@@ -726,9 +778,9 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_wave
   __shared__ int32_t found[W];
   extern __shared__ uint16_t list[];          // nbk entries
 
-  const int32_t whole = a.row_order ? a.row_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
-  const int32_t item = SPLIT ? whole / a.parts : whole, part = SPLIT ? whole - item * a.parts : 0;
-  const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
+  const Piece<SHARE> piece(a.row_pieces, a.parts);
+  if (piece.none()) return;
+  const int32_t bh = piece.item / a.nbq, qb = piece.item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
   const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
   const int h = lane >> 5, r32 = lane & 31;
@@ -740,9 +792,9 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_wave
   const uint8_t* kept = a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk;
   int32_t nu = kept_list<W>(a.nbk, list, found, [&](int32_t i) { return kept[i] ? i : -1; });
   int32_t first = 0;
-  if constexpr (SPLIT) {
-    first = (int32_t)((int64_t)nu * part / a.parts);
-    nu = (int32_t)((int64_t)nu * (part + 1) / a.parts) - first;
+  if constexpr (SHARE != Share::kWhole) {
+    first = part_start(nu, piece.part, piece.parts);
+    nu = part_start(nu, piece.part + 1, piece.parts) - first;
   }
   auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[first + i]); };
   DmaPlan<D, BLK> plan;
@@ -815,8 +867,9 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_wave
         out[(j * 4 + x) * 64][e] = grp == 0 ? dq[DH + j][4 * x + e] : dq[j][4 * x + e];
   __syncthreads();
   const f32x4* in = slot((1 - grp) * T::kWaves + gw);
-  if (SPLIT || row < n_q) {
-    const int64_t dst = (SPLIT ? (int64_t)whole * BLK + gw * 32 + r32 : (int64_t)bh * n_q + row) * D + 32 * DH * grp + 4 * h;
+  const bool partial = piece.partial();
+  if (partial || row < n_q) {
+    const int64_t dst = (partial ? (int64_t)piece.tile * BLK + gw * 32 + r32 : (int64_t)bh * n_q + row) * D + 32 * DH * grp + 4 * h;
 #pragma unroll
     for (int j = 0; j < DH; j++) {
       f32x16 v;
@@ -825,17 +878,13 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_wave
 #pragma unroll
         for (int e = 0; e < 4; e++)
           v[4 * x + e] = (grp == 0 ? dq[j][4 * x + e] : dq[DH + j][4 * x + e]) + in[(j * 4 + x) * 64][e];
-      if constexpr (SPLIT)
+      if (partial)
         store_cols(a.part_q + dst + 32 * j, v);
       else
         store_cols(a.dq + dst + 32 * j, v, a.scale);
     }
   }
 }
-
-// How dk's and dv's key blocks are shared out: one workgroup each; head_parts * list_parts workgroups each, the query heads
-// first (few blocks); or as order_cols says (many).
-enum class Share { kWhole, kParts, kOrder };
 
 template <int D, int BLK, Share SHARE>
 __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_dkv_kernel(MapArgs a) {
@@ -847,21 +896,9 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ int32_t found[W];
   extern __shared__ uint16_t list[];          // nbq entries
 
-  int32_t item, part = 0, parts = 1, tile = 0;             // tile: of the parts' sums
-  if constexpr (SHARE == Share::kOrder) {
-    const int2 e = a.col_order[blockIdx.x];
-    if (e.x < 0) return;
-    item = e.x;
-    part = e.y >> 16;
-    parts = e.y & 0xffff;
-    tile = blockIdx.x;
-  } else {
-    tile = item_of(blockIdx.x, gridDim.x);
-    if constexpr (SHARE == Share::kParts) parts = a.head_parts * a.list_parts;
-    item = tile / parts;
-    part = tile - item * parts;
-  }
-  const int32_t bk = item / a.nbk, kb = item - bk * a.nbk, n_kv = a.n_heads / a.group;
+  const Piece<SHARE> piece(a.col_pieces, a.head_parts * a.list_parts);
+  if (piece.none()) return;
+  const int32_t bk = piece.item / a.nbk, kb = piece.item - bk * a.nbk, n_kv = a.n_heads / a.group;
   const int32_t b = bk / n_kv, hk = bk - b * n_kv;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
   const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
@@ -882,18 +919,17 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const LaneAt<D> at_lane(lane);
 
   // the query heads of this workgroup, and its part of each one's list, or of all their lists one behind the other
-  int32_t hd0 = hk * a.group, hd1 = hd0 + a.group, lp = 0;
+  int32_t hd0 = hk * a.group, hd1 = hd0 + a.group, lp = 0, lo = 0, hi = 0;
   if constexpr (SHARE == Share::kParts) {
-    const int32_t hp = part / a.list_parts;
-    lp = part - hp * a.list_parts;
+    const int32_t hp = piece.part / a.list_parts;
+    lp = piece.part - hp * a.list_parts;
     hd1 = hd0 + a.group * (hp + 1) / a.head_parts;
     hd0 += a.group * hp / a.head_parts;
   }
-  int32_t lo = 0, hi = 0;
   if constexpr (SHARE == Share::kOrder) {
-    const int64_t all = a.col_counts[item];
-    lo = (int32_t)(all * part / parts);
-    hi = (int32_t)(all * (part + 1) / parts);
+    const int32_t all = a.col_counts[piece.item];
+    lo = part_start(all, piece.part, piece.parts);
+    hi = part_start(all, piece.part + 1, piece.parts);
   }
   for (int32_t hd = hd0; hd < hd1; hd++) {
     if (SHARE == Share::kOrder && hi <= 0) break;
@@ -907,8 +943,8 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
     int32_t nu = kept_list<W>(a.nbq, list, found, [&](int32_t i) { return kept[(int64_t)i * a.nbk] ? i : -1; });
     int32_t first = 0;
     if constexpr (SHARE == Share::kParts) {
-      first = (int32_t)((int64_t)nu * lp / a.list_parts);
-      nu = (int32_t)((int64_t)nu * (lp + 1) / a.list_parts) - first;
+      first = part_start(nu, lp, a.list_parts);
+      nu = part_start(nu, lp + 1, a.list_parts) - first;
     }
     if constexpr (SHARE == Share::kOrder) {
       const int32_t len = nu;
@@ -973,9 +1009,9 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
         out[(j * 4 + x) * 64][e] = grp == 0 ? dk[j][4 * x + e] : dv[j][4 * x + e];
   __syncthreads();
   const f32x4* in = slot((1 - grp) * T::kWaves + gw);
-  const bool partial = SHARE != Share::kWhole && parts > 1;
+  const bool partial = piece.partial();
   if (partial || key < n_k) {
-    const int64_t dst = (partial ? (int64_t)tile * BLK + gw * 32 + r32 : (int64_t)bk * n_k + key) * D + 4 * h;
+    const int64_t dst = (partial ? (int64_t)piece.tile * BLK + gw * 32 + r32 : (int64_t)bk * n_k + key) * D + 4 * h;
 #pragma unroll
     for (int j = 0; j < T::DT; j++) {
       f32x16 t;
@@ -992,55 +1028,38 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
-// out = scale * the sum of the parts of every row, of up to two tensors alike.  D / 4 lanes a row.
-struct PartSums {
-  const float* part[2];
-  __bf16* out[2];
-  float scale[2];
-  int32_t heads, n, nb, parts;      // rows: `heads` x n, in nb blocks each
+// The sums of what several workgroups left of an item, of dk, dv and dq as far as these have any; a workgroup adds 1024
+// columns of 16 bytes.
+struct Sums {
+  const float* part;
+  __bf16* out;
+  const int4* split;                // the items and their parts, or null: `parts` of every item
+  float scale;
+  int32_t items, parts, n, nb;      // items: all of them, or at most these are split; rows: n in nb blocks per head
+};
+struct AllSums {
+  Sums of[3];
 };
 template <int D, int BLK>
-__global__ __launch_bounds__(256) void psa_mapped_sum_kernel(PartSums p) {
-  constexpr int L = D / 4;
-  const int64_t r = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-  if (r >= (int64_t)p.heads * p.n) return;
-  const int c = threadIdx.x % L, which = blockIdx.y;
-  const int32_t head = (int32_t)(r / p.n), row = (int32_t)(r - (int64_t)head * p.n), blk = row / BLK;
-  const float* src = p.part[which] + (((int64_t)head * p.nb + blk) * p.parts * BLK + (row - blk * BLK)) * D + 4 * c;
-  f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int i = 0; i < p.parts; i++) s += *(const f32x4*)(src + (int64_t)i * BLK * D);
-  *(bf16x4*)(p.out[which] + r * D + 4 * c) = __builtin_convertvector(s * p.scale[which], bf16x4);
-}
-
-// dk and dv of the key blocks that went in pieces, four 16-byte columns a thread.
-template <int D, int BLK>
-__global__ __launch_bounds__(256) void psa_mapped_piece_sum_kernel(MapArgs a) {
-  constexpr int L = D / 4;
-  if ((int32_t)blockIdx.x >= a.col_split[-1].x) return;
-  const int4 e = a.col_split[blockIdx.x];
-  const bool values = blockIdx.y & 1;
-  const int32_t bk = e.x / a.nbk, key0 = (e.x - bk * a.nbk) * BLK;
-  const f32x4* src = (const f32x4*)(values ? a.part_v : a.part_k) + (int64_t)e.y * (BLK * L);
-  __bf16* dst = (values ? a.dv : a.dk) + ((int64_t)bk * a.n_k + key0) * D;
+__global__ __launch_bounds__(256) void psa_mapped_sum_kernel(AllSums all) {
+  constexpr int L = D / 4, kGroups = BLK * L / 1024;
+  const Sums p = all.of[blockIdx.y / kGroups];
+  const int32_t i = blockIdx.x;
+  if (i >= (p.split ? min(p.items, p.split[-1].x) : p.items)) return;
+  const int4 e = p.split ? p.split[i] : make_int4(i, i * p.parts, p.parts, 0);
+  const int32_t head = e.x / p.nb, row0 = (e.x - head * p.nb) * BLK;
+  const f32x4* src = (const f32x4*)p.part + (int64_t)e.y * (BLK * L);
+  __bf16* dst = p.out + ((int64_t)head * p.n + row0) * D;
   f32x4 s[4] = {};
-  const int at = (blockIdx.y >> 1) * 1024 + threadIdx.x;
+  const int at = blockIdx.y % kGroups * 1024 + threadIdx.x;
 #pragma unroll 2
-  for (int i = 0; i < e.z; i++)
+  for (int x = 0; x < e.z; x++)
 #pragma unroll
-    for (int u = 0; u < 4; u++) s[u] += src[(int64_t)i * (BLK * L) + at + 256 * u];
+    for (int u = 0; u < 4; u++) s[u] += src[(int64_t)x * (BLK * L) + at + 256 * u];
 #pragma unroll
   for (int u = 0; u < 4; u++)
-    if (key0 + (at + 256 * u) / L < a.n_k)
-      *(bf16x4*)(dst + 4 * (at + 256 * u)) = __builtin_convertvector(s[u] * (values ? 1.0f : a.scale), bf16x4);
-}
-
-template <int D, int BLK>
-hipError_t launch_sums(const PartSums& p, int tensors, hipStream_t stream) {
-  const int64_t rows = (int64_t)p.heads * p.n;
-  hipLaunchKernelGGL((psa_mapped_sum_kernel<D, BLK>), dim3((uint32_t)((rows * (D / 4) + 255) / 256), tensors), dim3(256), 0,
-                     stream, p);
-  return hipGetLastError();
+    if (row0 + (at + 256 * u) / L < p.n)
+      *(bf16x4*)(dst + 4 * (at + 256 * u)) = __builtin_convertvector(s[u] * p.scale, bf16x4);
 }
 
 // Whether the items are more than the workgroups that run at once (one of 128 rows to a CU, two of 64).
@@ -1087,64 +1106,82 @@ MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, i
   return l;
 }
 
+// The order of a backward kernel's `items`, whose lists hold at most `longest` blocks and would else go in `parts` each.
+// Items that all run at once are ordered too if a part may last long: the order costs 10 to 20 us of a balanced call, a
+// block of 64 takes 1.2 us and one of 128 2.4.  (D 128, blocks of 64, equal parts and the order, in us: 4 heads over 2 x 7791
+// with 226 of text, 31 kept, 337 and 230; without text 4 over 2 x 5760, 43 kept, 171 and 189; 3 heads x 2430 in a batch of
+// 4, whose lists stay below, 130 and 160.)
+Pieces pieces_for(int64_t items, int64_t longest, int32_t parts, int32_t block) {
+  Pieces p = {};
+  const int64_t room = room_of(block);
+  if (!ordered(items, block) && longest / parts * block <= 24 * 128) return p;
+  p.pieces = (int32_t)std::min(3 * room, items * ((longest + kFewBlocks - 1) / kFewBlocks));
+  p.splits = (int32_t)std::min(room, items);
+  p.grid = (int32_t)(items + p.pieces);
+  return p;
+}
+
 MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
-  const size_t rows = up256((size_t)n_bh * nbq * block * sizeof(float));
-  const size_t q_items = up256((size_t)n_bh * nbq * sizeof(int32_t)), k_items = up256((size_t)n_kv * nbk * sizeof(int32_t));
-  const bool by_col = ordered((int64_t)n_kv * nbk, block);
-  const int32_t pieces = max_pieces(room_of(block));
-  const size_t tile = (size_t)block * head_dim * sizeof(float);
-  MapBwdLayout l;
-  // dq's lists are shared out as the forward's; dk's and dv's over the query heads of a key head first
-  l.parts = map_parts(n_bh, nbq, nbk, block);
+  MapBwdLayout l = {};
+  // dq's lists go in parts as the forward's do, dk's and dv's by the query heads of a key head first; or in pieces.
   const int32_t group = n_bh / n_kv, room = std::max(1, (int32_t)(room_of(block) / ((int64_t)n_kv * nbk)));
+  l.parts = map_parts(n_bh, nbq, nbk, block);
   l.head_parts = std::min(group, room);
   l.list_parts = std::max(1, std::min(room / l.head_parts, nbq / 6));
   const int32_t kv_parts = l.head_parts * l.list_parts;
-  const size_t part_q = l.parts > 1 ? up256(tile * n_bh * nbq * l.parts) : 0;
-  const size_t part_kv = by_col ? up256(tile * pieces) : kv_parts > 1 ? up256(tile * n_kv * nbk * kv_parts) : 0;
-  l.neg_delta = rows;
-  l.row_counts = l.neg_delta + rows;
-  l.row_order = l.row_counts + q_items;
-  l.col_counts = l.row_order + q_items;
-  l.col_order = l.col_counts + k_items;
-  l.col_split = l.col_order + (by_col ? up256(((size_t)n_kv * nbk + pieces) * sizeof(int2)) : 0);
-  l.part_q = l.col_split + (by_col ? up256((1 + max_split(room_of(block))) * sizeof(int4)) : 0);
-  l.part_k = l.part_q + part_q;
-  l.part_v = l.part_k + part_kv;
-  l.total = l.part_v + part_kv;
+  l.rows = pieces_for((int64_t)n_bh * nbq, nbk, l.parts, block);
+  l.cols = pieces_for((int64_t)n_kv * nbk, (int64_t)group * nbq, kv_parts, block);
+  const size_t tile = (size_t)block * head_dim * sizeof(float);
+  auto take = [&](size_t& at, size_t bytes) {
+    at = l.total;
+    l.total += up256(bytes);
+  };
+  take(l.neg_lse2, (size_t)n_bh * nbq * block * sizeof(float));
+  take(l.neg_delta, (size_t)n_bh * nbq * block * sizeof(float));
+  if (l.rows.grid) {
+    take(l.row_counts, (size_t)n_bh * nbq * sizeof(int32_t));
+    take(l.row_order, l.rows.grid * sizeof(int2));
+    take(l.row_split, (1 + (size_t)l.rows.splits) * sizeof(int4));
+  }
+  if (l.cols.grid) {
+    take(l.col_counts, (size_t)n_kv * nbk * sizeof(int32_t));
+    take(l.col_order, l.cols.grid * sizeof(int2));
+    take(l.col_split, (1 + (size_t)l.cols.splits) * sizeof(int4));
+  }
+  const size_t tiles_q = l.rows.grid ? l.rows.pieces : l.parts > 1 ? (size_t)n_bh * nbq * l.parts : 0;
+  const size_t tiles_kv = l.cols.grid ? l.cols.pieces : kv_parts > 1 ? (size_t)n_kv * nbk * kv_parts : 0;
+  take(l.part_q, tile * tiles_q);
+  take(l.part_k, tile * tiles_kv);
+  take(l.part_v, tile * tiles_kv);
   return l;
 }
 
-// What comes before the main kernels: a backward call's row values, and the orders of the rows and columns that outnumber
-// the workgroups (the pointers of the others are cleared).
-static hipError_t launch_prepare(MapArgs& a, int32_t head_dim, bool backward, hipStream_t stream) {
+// What comes before the main kernels: a backward call's row values, the list lengths and the orders of the rows and columns
+// that have one.
+template <int D>
+static hipError_t launch_prepare(const MapArgs& a, bool backward, hipStream_t stream) {
   const int32_t n_kv = a.n_bh / a.group;
-  const bool by_row = ordered((int64_t)a.n_bh * a.nbq, a.block), by_col = backward && ordered((int64_t)n_kv * a.nbk, a.block);
-  if (!by_row) a.row_order = nullptr;
-  if (!by_col) a.col_order = nullptr;
-  if (!by_row || backward || a.block != 64) a.paired = a.pair_counts = nullptr;
-  const int64_t value_groups = backward ? ((int64_t)a.n_bh * a.nbq * a.block * (head_dim / 8) + 255) / 256 : 0;
-  const int32_t row_groups = by_row ? (a.n_bh * pairs_per_head(a.nbq) + 3) / 4 : 0;
-  const int64_t col_groups = by_col ? (int64_t)(a.nbk + 63) / 64 * n_kv : 0;
+  const int64_t value_groups = backward ? ((int64_t)a.n_bh * a.nbq * a.block * (D / 8) + 255) / 256 : 0;
+  const int32_t row_groups = a.row_counts ? (a.n_bh * pairs_per_head(a.nbq) + 3) / 4 : 0;
+  const int64_t col_groups = a.col_counts ? (int64_t)(a.nbk + 63) / 64 * n_kv : 0;
   const int64_t groups = value_groups + row_groups + col_groups;
   if (groups == 0) return hipSuccess;
-  auto kernel = head_dim == 128 ? psa_mapped_prepare_kernel<128> : psa_mapped_prepare_kernel<64>;
-  hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(256), 0, stream, a, (int32_t)value_groups, row_groups);
+  hipLaunchKernelGGL(psa_mapped_prepare_kernel<D>, dim3((uint32_t)groups), dim3(256), 0, stream, a, (int32_t)value_groups,
+                     row_groups);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || (!by_row && !by_col)) return e;
-  hipLaunchKernelGGL(psa_mapped_order_kernel, dim3(by_row && (by_col || a.paired) ? 2 : 1), dim3(kOrderThreads), 0, stream, a,
-                     by_row ? Order::kRows : Order::kCols, by_col ? Order::kCols : Order::kPairs, head_dim,
-                     room_of(a.block));
+  if (e != hipSuccess || (!a.row_counts && !a.col_counts)) return e;
+  const Order row = backward ? Order::kRowPieces : Order::kRows, other = backward ? Order::kColPieces : Order::kPairs;
+  const bool both = a.row_counts && (backward ? a.col_counts != nullptr : a.paired != nullptr);
+  hipLaunchKernelGGL(psa_mapped_order_kernel, dim3(both ? 2 : 1), dim3(kOrderThreads), 0, stream, a,
+                     a.row_counts ? row : other, other, D, room_of(a.block));
   return hipGetLastError();
 }
 
-hipError_t launch_map_fwd(const MapArgs& args, int32_t head_dim, hipStream_t stream) {
-  MapArgs a = args;
-  if (a.parts > 1) a.row_order = a.paired = nullptr;
-  const hipError_t e = a.parts == 1 ? launch_prepare(a, head_dim, false, stream) : hipSuccess;
-  if (e != hipSuccess) return e;
+hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream) {
   return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
     constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
+    hipError_t e = launch_prepare<D>(a, false, stream);
+    if (e != hipSuccess) return e;
     const dim3 grid(a.n_bh * a.nbq * a.parts);
     if (a.parts == 1) {
       if constexpr (B == 64) {
@@ -1156,7 +1193,7 @@ hipError_t launch_map_fwd(const MapArgs& args, int32_t head_dim, hipStream_t str
       return hipGetLastError();
     }
     hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, true>), grid, dim3(4 * B), list_bytes(a.nbk), stream, a);
-    const hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
     constexpr int kLanes = D / 4, kSide = 256 / kLanes;
     const int32_t rows = a.n_bh * a.n_q;
@@ -1168,44 +1205,48 @@ hipError_t launch_map_fwd(const MapArgs& args, int32_t head_dim, hipStream_t str
   });
 }
 
-hipError_t launch_map_bwd(const MapArgs& args, int32_t head_dim, hipStream_t stream) {
-  MapArgs a = args;
-  hipError_t e = launch_prepare(a, head_dim, true, stream);
-  if (e != hipSuccess) return e;
+hipError_t launch_map_bwd(const MapArgs& a, int32_t head_dim, hipStream_t stream) {
   return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
     constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
-    hipError_t e = hipSuccess;
-    const int32_t n_kv = a.n_bh / a.group, kv_parts = a.head_parts * a.list_parts;
-    if (a.col_order) {
-      const int32_t room = room_of(B);
-      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, Share::kOrder>), dim3(n_kv * a.nbk + max_pieces(room)), dim3(4 * B),
-                         list_bytes(a.nbq), stream, a);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((psa_mapped_piece_sum_kernel<D, B>), dim3(max_split(room), 2 * (B * D / 4096)), dim3(256), 0, stream,
-                         a);
-      e = hipGetLastError();
-    } else if (kv_parts == 1) {
-      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, Share::kWhole>), dim3(n_kv * a.nbk), dim3(4 * B), list_bytes(a.nbq),
-                         stream, a);
-      e = hipGetLastError();
-    } else {
-      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, Share::kParts>), dim3(n_kv * a.nbk * kv_parts), dim3(4 * B),
-                         list_bytes(a.nbq), stream, a);
-      e = hipGetLastError();
-      if (e == hipSuccess)
-        e = launch_sums<D, B>({{a.part_k, a.part_v}, {a.dk, a.dv}, {a.scale, 1.0f}, n_kv, a.n_k, a.nbk, kv_parts}, 2, stream);
-    }
+    hipError_t e = launch_prepare<D>(a, true, stream);
     if (e != hipSuccess) return e;
-    if (a.parts == 1) {
-      hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B, false>), dim3(a.n_bh * a.nbq), dim3(4 * B), list_bytes(a.nbk), stream, a);
-      return hipGetLastError();
-    }
-    hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B, true>), dim3(a.n_bh * a.nbq * a.parts), dim3(4 * B), list_bytes(a.nbk),
-                       stream, a);
+    const int32_t n_kv = a.n_bh / a.group, rows = a.n_bh * a.nbq, cols = n_kv * a.nbk, kv_parts = a.head_parts * a.list_parts;
+    const dim3 threads(4 * B);
+    const bool row_order = a.row_pieces.grid > 0, col_order = a.col_pieces.grid > 0;
+    if (col_order)
+      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, Share::kOrder>), dim3(a.col_pieces.grid), threads, list_bytes(a.nbq),
+                         stream, a);
+    else if (kv_parts > 1)
+      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, Share::kParts>), dim3(cols * kv_parts), threads, list_bytes(a.nbq), stream,
+                         a);
+    else
+      hipLaunchKernelGGL((psa_mapped_dkv_kernel<D, B, Share::kWhole>), dim3(cols), threads, list_bytes(a.nbq), stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return launch_sums<D, B>({{a.part_q, nullptr}, {a.dq, nullptr}, {a.scale, 0.0f}, a.n_bh, a.n_q, a.nbq, a.parts}, 1, stream);
+    if (row_order)
+      hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B, Share::kOrder>), dim3(a.row_pieces.grid), threads, list_bytes(a.nbk),
+                         stream, a);
+    else if (a.parts > 1)
+      hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B, Share::kParts>), dim3(rows * a.parts), threads, list_bytes(a.nbk), stream,
+                         a);
+    else
+      hipLaunchKernelGGL((psa_mapped_dq_kernel<D, B, Share::kWhole>), dim3(rows), threads, list_bytes(a.nbk), stream, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    AllSums sums;
+    int32_t n = 0, most = 0;
+    auto sum = [&](const float* part, __bf16* out, const Pieces& p, float scale, int32_t items, int32_t parts, int32_t len,
+                   int32_t nb) {
+      if (!p.grid && parts == 1) return;
+      sums.of[n] = {part, out, p.split, scale, p.grid ? p.splits : items, parts, len, nb};
+      most = std::max(most, sums.of[n++].items);
+    };
+    sum(a.part_k, a.dk, a.col_pieces, a.scale, cols, kv_parts, a.n_k, a.nbk);
+    sum(a.part_v, a.dv, a.col_pieces, 1.0f, cols, kv_parts, a.n_k, a.nbk);
+    sum(a.part_q, a.dq, a.row_pieces, a.scale, rows, a.parts, a.n_q, a.nbq);
+    if (n == 0) return hipSuccess;
+    hipLaunchKernelGGL((psa_mapped_sum_kernel<D, B>), dim3(most, n * (B * D / 4096)), dim3(256), 0, stream, sums);
+    return hipGetLastError();
   });
 }
 

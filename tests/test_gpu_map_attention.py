@@ -181,6 +181,14 @@ def test_key_blocks_that_every_row_keeps(d, block, h, hk, nq, density):
 
 
 @pytest.mark.parametrize("d,block", SHAPES)
+@pytest.mark.parametrize("hk,density", [(8, 0.15), (4, 0.0)])
+def test_few_long_lists_of_other_lengths(d, block, hk, density):
+    """As many query and key blocks as run at once and fewer: a row and a column kept whole go in pieces."""
+    n = (56 if block == 64 else 31) * block
+    check(1, 8, hk, n - 9, n - 1, block, d, density=density, heads=[0, 7])
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
 @pytest.mark.parametrize("density", [0.0, 1.0])
 def test_empty_and_full_maps(d, block, density):
     nq, nk = 4, 6
