@@ -825,18 +825,19 @@ psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, i
   if (s != PSA_OK) return s;
   a.parts = l.parts;
   char* ws = (char*)workspace;
-  if (l.parts > 1) {
-    a.part_o = (float*)ws;
-    a.part_ml = (float2*)(ws + l.part_ml);
-  } else if (l.total) {
-    a.row_counts = (int32_t*)ws;
-    a.row_order = (int32_t*)(ws + l.row_order);
-    if (block == 64) {
+  a.row_pieces = l.rows;
+  if (l.rows.grid) {
+    a.row_counts = (int32_t*)(ws + l.row_counts);
+    a.row_pieces.order = (int2*)(ws + l.row_order);
+    a.row_pieces.split = (int4*)(ws + l.row_split) + 1;
+    if (l.paired) {
       a.pair_counts = (int32_t*)(ws + l.pair_counts);
       a.pair_order = (int32_t*)(ws + l.pair_order);
       a.paired = (int32_t*)(ws + l.paired);
     }
   }
+  a.part_o = (float*)(ws + l.part_o);
+  a.part_ml = (float2*)(ws + l.part_ml);
   const hipError_t e = psa::launch_map_fwd(a, head_dim, stream);
   return e == hipSuccess ? PSA_OK : hip_fail(e, "psa_attention_map_fwd launch");
 }

@@ -24,8 +24,8 @@ SelectLayout select_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t
 hipError_t launch_select(const SelectArgs& args, int32_t head_dim, hipStream_t stream);
 
 // Attention over a block map.
-// Order of a backward kernel's items (psa_map.hip, order_pieces): `grid` workgroups (0: there is none), of which at most
-// `pieces` take a piece of a list, of at most `splits` items.
+// Order of a kernel's items (psa_map.hip, order_pieces): `grid` workgroups (0: there is none), of which at most
+// `pieces` (0: the lists stay whole) take a piece of a list, of at most `splits` items.
 struct Pieces {
   int2* order;
   int4* split;
@@ -39,14 +39,14 @@ struct MapArgs {
   float* lse;                         // [n_bh][n_q] or null (backward: an input)
   const uint8_t* map;                 // [n_heads][nbq][nbk] per batch element
   int64_t map_stride_b, kv_stride_b, kv_stride_h;
-  float* part_o;                      // forward in parts: [n_bh][nbq][parts][block][d] and (m, l) of the rows
+  float* part_o;                      // forward: sums of a part of a list, [tile][block][d], and (m, l) of its rows
   float2* part_ml;
   float *neg_lse2, *neg_delta;        // backward: [n_bh][nbq][block]
-  int32_t *row_counts, *row_order;    // list lengths of the (head, query block) items (null: not ordered), their order
+  int32_t* row_counts;                // list lengths of the (head, query block) items (null: not ordered)
   int32_t *pair_counts, *pair_order;  // forward, block 64: those of pairs of query blocks, and
   int32_t* paired;                    // whether pairs run (null: they do not)
   int32_t* col_counts;                // backward: those of the (key head, key block) items
-  Pieces row_pieces, col_pieces;      // backward
+  Pieces row_pieces, col_pieces;
   int32_t n_bh, n_heads, group;       // group: query heads per key head
   float *part_q, *part_k, *part_v;    // backward: sums of a part of a list, [tile][block][d]
   int32_t n_q, n_k, nbq, nbk, block, parts;
@@ -55,9 +55,9 @@ struct MapArgs {
   float pow2, factor;                 // forward: c = pow2 factor, a power of two with c's sign and a factor in [1, 2)
 };
 struct MapLayout {
+  Pieces rows;                        // sizes alone
   int32_t parts;
-  size_t part_ml, total;              // in parts (part_o first)
-  size_t row_order, pair_counts, pair_order, paired;  // in one part (row_counts first)
+  size_t row_counts, row_order, row_split, pair_counts, pair_order, paired, part_o, part_ml, total;
 };
 MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);

@@ -82,8 +82,8 @@ __device__ __forceinline__ int32_t item_of(int32_t blk, int32_t items) {
 // `single` those that each keeps, over all pairs.  A wave waits while its neighbour's block alone is worked on, so
 // pairs pay where neighbours share enough; at head dim 64, whose four waves per SIMD cover such waits, in long lists
 // always.  Microseconds in pairs and one by one at either / single 0.88, 0.71 and 0.50:
-//   head dim 64   12 heads x 32760, density 0.25 (3072 pairs)  1102, 963, 861 and 1259, 1191, 1190
-//                 8 x 8000, 0.2 (504 pairs)                    81, 71, 58     and 69, 70, 70
+//   head dim 64   12 heads x 32760, density 0.25 (256 pairs each)  1102, 963, 861 and 1259, 1191, 1190
+//                 8 x 8000, 0.2 (63 pairs each)                81, 71, 58     and 69, 70, 70
 //   head dim 128  12 x 32760, 0.25                             2039, 1779, 1540 and 1840, 1820, 1822
 //                 8 x 8000, 0.2                                105, 88, 78    and 94, 94, 92
 constexpr int32_t kManyPairs = 2048;        // twice the workgroups that run at once
@@ -313,78 +313,88 @@ __device__ __forceinline__ int length_class(int32_t c, float mean) {
          x >= 1.25f * mean ? 4 : x >= 1.1f * mean ? 5 : x >= 0.9f * mean ? 6 : 7;
 }
 
-// row_order[workgroup] = (head, query block); for pairs of query blocks pair_order, and whether they pay (pairs_pay).
-__device__ __forceinline__ void order_rows(const MapArgs& a, bool pairs, int32_t head_dim, OrderSpace& s) {
-  const Items rows(a.row_counts, a.n_bh * a.nbq);
-  const Items items = pairs ? Items(a.pair_counts, a.n_bh * pairs_per_head(a.nbq)) : rows;
-  int32_t* order = pairs ? a.pair_order : a.row_order;
-  const unsigned long long work = items.sum(s.totals);
-  if (pairs) {
-    const unsigned long long single = rows.sum(s.totals);
-    if (threadIdx.x == 0) *a.paired = pairs_pay(work, single, items.n, head_dim) ? 1 : 0;
-  }
-  const float mean = (float)work / (float)items.n;
-  place_items(items, s.at, s.waves, [&](int32_t c) { return length_class(c, mean); },
-              [&](int32_t i, int32_t place) { order[place] = i; });
-}
-
-// The lists of the backward kernels: of a (key head, key block) item for dk and dv, of a (head, query block) item for
-// dq.  Their lengths differ: a block that every row keeps (text, the first block of a sequence) lists the rows of every
-// query head, a row of text lists every key block, and such a list can outlast all the others together.  So long ones go
-// in pieces, each to a workgroup of its own that leaves its sums in the workspace; psa_mapped_sum_kernel adds them.
+// The lists' lengths differ: a row of text lists every key block, a key block that every row keeps (text, the first block
+// of a sequence) lists the rows of every query head, and such a list can outlast all the others together.  So long
+// ones go in pieces, each to a workgroup of its own that leaves its sums in the workspace, where another kernel adds them.
 // With `room` workgroups sharing the work (`share` blocks each):
 //   * more items than room: lists longer than 1.25 share, in pieces of half a share, 8 blocks at least (shorter ones,
 //     started first, end with the others).  At most 0.8 room lists and 2.8 room pieces, whatever the map.
 //   * fewer: a list of average length goes in room / items pieces and a longer one in pieces as long, 4 blocks at
 //     least.  At most 4/3 room pieces.
-// Whole calls without and with pieces, in us.  Every row keeps the first block and others by chance: 12 heads x 32760
-// (D 128, blocks of 128, 8 kept) 1247 and 1031; 16 heads over 4 3815 and 1298; 12 x 16384 (D 64, blocks of 64, 12 kept)
-// 342 and 249; 32 over 8 x 16384 (D 128, blocks of 64, 16 kept) 2060 and 1280.  Rows of text (226 tokens): 8 heads x
-// 4096 (D 128, blocks of 64, 8 kept) 181 and 124.  Maps without any of these pay 0 to 2 %.
+// Whole gradients without and with pieces, in us.  Every row keeps the first block and others by chance: 12 heads x
+// 32760 (D 128, blocks of 128, 8 kept) 1247 and 1031; 16 heads over 4 3815 and 1298; 12 x 16384 (D 64, blocks of 64, 12
+// kept) 342 and 249; 32 over 8 x 16384 (D 128, blocks of 64, 16 kept) 2060 and 1280.  Rows of text (226 tokens): 8
+// heads x 4096 (D 128, blocks of 64, 8 kept) 181 and 124.  Maps without any of these pay 0 to 2 %.
+constexpr int kPieceBlocks = 8, kFewBlocks = 4;
+struct Cut {
+  float mean, piece, longest, up;
+  __device__ __forceinline__ Cut(unsigned long long work, int32_t items, int32_t room, const Pieces& to) {
+    const float share = (float)work / (float)room;
+    mean = (float)work / (float)items;
+    const bool few = items <= room;
+    piece = few ? fmaxf((float)kFewBlocks, mean / (float)(room / items)) : fmaxf((float)kPieceBlocks, 0.5f * share);
+    longest = to.pieces == 0 ? __builtin_inff() : few ? 1.5f * piece : fmaxf(1.5f * kPieceBlocks, 1.25f * share);
+    up = few ? 0.5f : 1.0f;
+  }
+  __device__ __forceinline__ bool cuts(int32_t c) const { return (float)c > longest; }
+  __device__ __forceinline__ int32_t pieces(int32_t c) const { return (int32_t)((float)c / piece + up); }     // of one that it cuts
+};
+
 //   order[workgroup] = (item, piece << 16 | pieces): the pieces first, then the whole items by their lengths, then -1
 //   split[i]         = (item, workgroup of its first piece, pieces), split[-1].x their number
-constexpr int kPieceBlocks = 8, kFewBlocks = 4;
 __device__ __forceinline__ void order_pieces(const Items& items, const Pieces& to, int32_t room, OrderSpace& s) {
-  const float work = (float)items.sum(s.totals), share = work / (float)room, mean = work / (float)items.n;
-  const bool few = items.n <= room;
-  const float piece = few ? fmaxf((float)kFewBlocks, mean / (float)(room / items.n)) : fmaxf((float)kPieceBlocks, 0.5f * share);
-  const float longest = few ? 1.5f * piece : fmaxf(1.5f * kPieceBlocks, 1.25f * share);
-  const float up = few ? 0.5f : 1.0f;
-  auto pieces_of = [&](int32_t c) { return (float)c > longest ? (int32_t)((float)c / piece + up) : 0; };
-  int32_t split = 0, pieces = 0, all_split, all_pieces;
-  items.each([&](int32_t, int32_t c) {
-    const int32_t p = pieces_of(c);
-    split += p > 0;
-    pieces += p;
-  });
-  split = sum_before(split, s.waves, &all_split);
-  pieces = sum_before(pieces, s.waves, &all_pieces);
-  if (threadIdx.x == 0) to.split[-1] = make_int4(all_split, 0, 0, 0);
-  items.each([&](int32_t i, int32_t c) {
-    const int32_t p = pieces_of(c);
-    if (p == 0) return;
-    to.split[split++] = make_int4(i, pieces, p, 0);
-    for (int32_t x = 0; x < p; x++) to.order[pieces++] = make_int2(i, x << 16 | p);
-  });
-  place_items(items, s.at, s.waves, [&](int32_t c) { return pieces_of(c) > 0 ? -1 : length_class(c, mean); },
+  const Cut cut(items.sum(s.totals), items.n, room, to);
+  int32_t split = 0, pieces = 0, all_split = 0, all_pieces = 0;
+  if (to.pieces) {
+    items.each([&](int32_t, int32_t c) {
+      if (!cut.cuts(c)) return;
+      split++;
+      pieces += cut.pieces(c);
+    });
+    split = sum_before(split, s.waves, &all_split);
+    pieces = sum_before(pieces, s.waves, &all_pieces);
+    if (threadIdx.x == 0) to.split[-1] = make_int4(all_split, 0, 0, 0);
+    if (all_split)
+      items.each([&](int32_t i, int32_t c) {
+        if (!cut.cuts(c)) return;
+        const int32_t p = cut.pieces(c);
+        to.split[split++] = make_int4(i, pieces, p, 0);
+        for (int32_t x = 0; x < p; x++) to.order[pieces++] = make_int2(i, x << 16 | p);
+      });
+  }
+  place_items(items, s.at, s.waves, [&](int32_t c) { return cut.cuts(c) ? -1 : length_class(c, cut.mean); },
               [&](int32_t i, int32_t place) { to.order[all_pieces + place] = make_int2(i, 1); });
   for (int32_t i = all_pieces + items.n - all_split + threadIdx.x; i < to.grid; i += kOrderThreads)
     to.order[i] = make_int2(-1, 0);
 }
 
-// Up to two orders, a workgroup each: the rows' and the pairs' of a forward call, the rows' and the columns' pieces of
-// a backward call.
-enum class Order { kRows, kPairs, kRowPieces, kColPieces };
+// Pairs of query blocks: pair_order[workgroup] = (head, pair), and whether they run: if they pay (pairs_pay) and no list
+// goes in pieces.
+__device__ __forceinline__ void order_pairs(const MapArgs& a, int32_t head_dim, int32_t room, OrderSpace& s) {
+  const Items rows(a.row_counts, a.n_bh * a.nbq), items(a.pair_counts, a.n_bh * pairs_per_head(a.nbq));
+  const unsigned long long single = rows.sum(s.totals), either = items.sum(s.totals);
+  const Cut cut(single, rows.n, room, a.row_pieces);
+  int32_t any = 0;
+  rows.each([&](int32_t, int32_t c) { any |= cut.cuts(c); });
+  any = __syncthreads_or(any);
+  if (threadIdx.x == 0) *a.paired = !any && pairs_pay(either, single, items.n, head_dim) ? 1 : 0;
+  const float mean = (float)either / (float)items.n;
+  place_items(items, s.at, s.waves, [&](int32_t c) { return length_class(c, mean); },
+              [&](int32_t i, int32_t place) { a.pair_order[place] = i; });
+}
+
+// Up to two orders, a workgroup each: the rows', and the pairs' of a forward call or the columns' of a backward call.
+enum class Order { kRows, kPairs, kCols };
 __global__ __launch_bounds__(kOrderThreads) void psa_mapped_order_kernel(MapArgs a, Order first, Order second,
                                                                          int32_t head_dim, int32_t room) {
   __shared__ OrderSpace space;
   const Order which = blockIdx.x == 0 ? first : second;
-  if (which == Order::kRowPieces)
+  if (which == Order::kRows)
     order_pieces(Items(a.row_counts, a.n_bh * a.nbq), a.row_pieces, room, space);
-  else if (which == Order::kColPieces)
+  else if (which == Order::kCols)
     order_pieces(Items(a.col_counts, a.n_bh / a.group * a.nbk), a.col_pieces, room, space);
   else
-    order_rows(a, which == Order::kPairs, head_dim, space);
+    order_pairs(a, head_dim, room, space);
 }
 
 // Where this lane reads a tile of rows of D channels in LDS, in bytes from the tile's start: `rows` for the operand of
@@ -518,13 +528,45 @@ __device__ __forceinline__ void store_cols(float* dst, const f32x16& v) {
   for (int a = 0; a < 4; a++) *(f32x4*)(dst + 8 * a) = f32x4{v[4 * a], v[4 * a + 1], v[4 * a + 2], v[4 * a + 3]};
 }
 
+// How a kernel's lists are shared out: a workgroup each; the same number of parts each; or as order_pieces
+// says.
+enum class Share { kWhole, kParts, kOrder };
+
+// A workgroup's item and its part of the item's list, whose sums go to `tile` of the workspace if there are several.
+template <Share SHARE>
+struct Piece {
+  int32_t item, part = 0, parts = 1, tile;
+  __device__ __forceinline__ Piece(const Pieces& order, int32_t equal_parts) {
+    if constexpr (SHARE == Share::kOrder) {
+      tile = blockIdx.x;
+      const int2 e = order.order[tile];
+      item = e.x;
+      part = e.y >> 16;
+      parts = e.y & 0xffff;
+    } else {
+      item = tile = item_of(blockIdx.x, gridDim.x);
+      if constexpr (SHARE == Share::kParts) {
+        parts = equal_parts;
+        item = tile / parts;
+        part = tile - item * parts;
+      }
+    }
+  }
+  __device__ __forceinline__ bool none() const { return SHARE == Share::kOrder && item < 0; }
+  __device__ __forceinline__ bool partial() const { return SHARE != Share::kWhole && parts > 1; }
+};
+// Where a part of a list of n starts.
+__device__ __forceinline__ int32_t part_start(int32_t n, int32_t part, int32_t parts) {
+  return (int32_t)((int64_t)n * part / parts);
+}
+
 // ---------------------------------------------------------------------------------------------
 // Forward.
 // ---------------------------------------------------------------------------------------------
 
-// SPLIT: few query blocks; `parts` workgroups share one, each takes a part of its list and leaves its sums
-// (relative to its base m, with m and l) in the workspace, where psa_mapped_join_kernel adds them.
-template <int D, int BLK, bool SPLIT>
+// A workgroup that takes a part of a list leaves its sums (relative to its base m, with m and l) in the workspace, where
+// psa_mapped_join_kernel adds them.
+template <int D, int BLK, Share SHARE>
 __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_fwd_kernel(MapArgs a) {
   using T = Tile<D, BLK>;
   constexpr int HK = BLK / 2, W = 2 * T::kWaves, DH = T::DT / 2;
@@ -535,10 +577,11 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ float2 stat[W][32];              // (m, l) of every wave's rows
   extern __shared__ uint16_t list[];          // nbk entries
 
-  if (BLK == 64 && !SPLIT && a.paired && *a.paired) return;   // (psa_mapped_pairs_kernel runs)
-  const int32_t whole = a.row_order ? a.row_order[blockIdx.x] : item_of(blockIdx.x, gridDim.x);
-  const int32_t item = SPLIT ? whole / a.parts : whole, part = SPLIT ? whole - item * a.parts : 0;
-  const int32_t bh = item / a.nbq, qb = item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
+  if (BLK == 64 && SHARE == Share::kOrder && a.paired && *a.paired) return;   // (psa_mapped_pairs_kernel runs)
+  const Piece<SHARE> piece(a.row_pieces, a.parts);
+  if (piece.none()) return;
+  const bool partial = piece.partial();
+  const int32_t bh = piece.item / a.nbq, qb = piece.item - bh * a.nbq, b = bh / a.n_heads, hd = bh - b * a.n_heads;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, gw = wave & (T::kWaves - 1);
   const int grp = __builtin_amdgcn_readfirstlane(wave / T::kWaves);
   const int h = lane >> 5, r32 = lane & 31;
@@ -552,9 +595,9 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const uint8_t* kept = a.map + b * a.map_stride_b + ((int64_t)hd * a.nbq + qb) * a.nbk;
   int32_t nu = kept_list<W>(a.nbk, list, found, [&](int32_t i) { return kept[i] ? i : -1; });
   int32_t first = 0;
-  if constexpr (SPLIT) {
-    first = (int32_t)((int64_t)nu * part / a.parts);
-    nu = (int32_t)((int64_t)nu * (part + 1) / a.parts) - first;
+  if constexpr (SHARE != Share::kWhole) {
+    first = part_start(nu, piece.part, piece.parts);
+    nu = part_start(nu, piece.part + 1, piece.parts) - first;
   }
   auto entry = [&](int i) { return (int)__builtin_amdgcn_readfirstlane(list[first + i]); };
 
@@ -613,7 +656,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const float alpha = st.m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((st.m - top) * a.factor);
   const float beta = other.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((other.x - top) * a.factor);
   const float lsum = mine * alpha + other.y * beta;
-  const float inv = SPLIT ? 1.0f : lsum > 0.0f ? 1.0f / lsum : 0.0f;
+  const float inv = partial ? 1.0f : lsum > 0.0f ? 1.0f / lsum : 0.0f;
   static_assert(W * DH * 4096 <= 4 * T::BYTES, "a wave's half of O fits its share of the buffers");
   constexpr int kPer = T::BYTES / (DH * 4096);            // waves per buffer
   auto slot = [&](int w) { return (f32x4*)((w / kPer < 2 ? sk[w / kPer] : sv[w / kPer - 2]) + (w % kPer) * DH * 4096) + lane; };
@@ -629,7 +672,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   __syncthreads();
   const f32x4* in = slot((1 - grp) * T::kWaves + gw);
-  const int64_t place = SPLIT ? (int64_t)whole * BLK + gw * 32 + r32 : (int64_t)bh * n_q + row;
+  const int64_t place = partial ? (int64_t)piece.tile * BLK + gw * 32 + r32 : (int64_t)bh * n_q + row;
   const int64_t at = place * D + 32 * DH * grp + 4 * h;
 #pragma unroll
   for (int j = 0; j < DH; j++)
@@ -640,14 +683,14 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const f32x4 lower = {lo[e], lo[e + 1], lo[e + 2], lo[e + 3]}, upper = {hi[e], hi[e + 1], hi[e + 2], hi[e + 3]};
       const f32x4 sum = ((grp == 0 ? lower : upper) * alpha + in[(j * 4 + x) * 64]) * inv;
       if (row < n_q) {
-        if constexpr (SPLIT)
+        if (partial)
           *(f32x4*)(a.part_o + at + 32 * j + 8 * x) = sum;
         else
           *(bf16x4*)(a.o + at + 32 * j + 8 * x) = __builtin_convertvector(sum, bf16x4);
       }
     }
   if (grp == 0 && h == 0 && row < n_q) {
-    if constexpr (SPLIT)
+    if (partial)
       a.part_ml[place] = make_float2(top, lsum);
     else if (a.lse)
       a.lse[place] = lsum > 0.0f ? (top * a.factor + __builtin_log2f(lsum)) * kLn2 : -__builtin_inff();
@@ -689,17 +732,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4
 // Adds the parts of a query row: o = sum_p 2^(f (m_p - m)) O_p / sum_p 2^(f (m_p - m)) l_p.  D / 4 lanes for a row's
 // channels, G of these side by side for its parts: one where parts are few and rows many (10400 rows in three parts:
 // 4 us less than with a workgroup a row), else all 256 / (D / 4) of a workgroup (one lane for all 64 parts of
-// a single token took 15 us).
-template <int D, int BLK, int G>
+// a single token took 15 us).  The lists that order_pieces cut have a lane each, a workgroup R rows.
+template <int D, int BLK, Share SHARE, int G>
 __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
   constexpr int L = D / 4, R = 256 / (L * G);
   __shared__ f32x4 sum_o[G > 1 ? G : 1][L];
   __shared__ float2 sum_ml[G];
-  const int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / (L * G);
-  if (r >= (int64_t)a.n_bh * a.n_q) return;
   const int c = threadIdx.x % L, g = threadIdx.x / L % G;
-  const int32_t bh = (int32_t)(r / a.n_q), row = (int32_t)(r - (int64_t)bh * a.n_q), qb = row / BLK;
-  const int64_t first = ((int64_t)bh * a.nbq + qb) * a.parts * BLK + (row - qb * BLK);
+  int64_t r, first;                       // the row, its place in the first part
+  int32_t parts = a.parts;
+  if constexpr (SHARE == Share::kOrder) {
+    if ((int32_t)blockIdx.x >= min(a.row_pieces.splits, a.row_pieces.split[-1].x)) return;
+    const int4 e = a.row_pieces.split[blockIdx.x];
+    const int32_t bh = e.x / a.nbq, x = blockIdx.y * R + threadIdx.x / L, row = (e.x - bh * a.nbq) * BLK + x;
+    if (row >= a.n_q) return;
+    r = (int64_t)bh * a.n_q + row;
+    first = (int64_t)e.y * BLK + x;
+    parts = e.z;
+  } else {
+    r = (int64_t)blockIdx.x * R + threadIdx.x / (L * G);
+    if (r >= (int64_t)a.n_bh * a.n_q) return;
+    const int32_t bh = (int32_t)(r / a.n_q), row = (int32_t)(r - (int64_t)bh * a.n_q), qb = row / BLK;
+    first = ((int64_t)bh * a.nbq + qb) * parts * BLK + (row - qb * BLK);
+  }
   float m = -__builtin_inff(), l = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   auto add = [&](float pm, float pl, f32x4 po) {
@@ -711,7 +766,7 @@ __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
     m = top;
   };
 #pragma unroll 4
-  for (int p = g; p < a.parts; p += G) {
+  for (int p = g; p < parts; p += G) {
     const int64_t at = first + (int64_t)p * BLK;
     const float2 ml = a.part_ml[at];
     add(ml.x, ml.y, *(const f32x4*)(a.part_o + at * D + 4 * c));
@@ -736,38 +791,6 @@ __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
 // Waves per SIMD of dq's kernel: at head dim 64 the registers allow more than two, and no unit alone bounds it (12 heads
 // x 16000, dq, dk and dv: block 64 784 us with two, 761 with three, 783 with four; block 128 761, 759, 740).
 constexpr int dq_waves(int d, int blk) { return d == 128 ? 2 : blk == 64 ? 3 : 4; }
-
-// How the lists of a backward kernel are shared out: a workgroup each; the same number of parts each; or as order_pieces
-// says.
-enum class Share { kWhole, kParts, kOrder };
-
-// A workgroup's item and its part of the item's list, whose sums go to `tile` of the workspace if there are several.
-template <Share SHARE>
-struct Piece {
-  int32_t item, part = 0, parts = 1, tile;
-  __device__ __forceinline__ Piece(const Pieces& order, int32_t equal_parts) {
-    if constexpr (SHARE == Share::kOrder) {
-      tile = blockIdx.x;
-      const int2 e = order.order[tile];
-      item = e.x;
-      part = e.y >> 16;
-      parts = e.y & 0xffff;
-    } else {
-      item = tile = item_of(blockIdx.x, gridDim.x);
-      if constexpr (SHARE == Share::kParts) {
-        parts = equal_parts;
-        item = tile / parts;
-        part = tile - item * parts;
-      }
-    }
-  }
-  __device__ __forceinline__ bool none() const { return SHARE == Share::kOrder && item < 0; }
-  __device__ __forceinline__ bool partial() const { return SHARE != Share::kWhole && parts > 1; }
-};
-// Where a part of a list of n starts.
-__device__ __forceinline__ int32_t part_start(int32_t n, int32_t part, int32_t parts) {
-  return (int32_t)((int64_t)n * part / parts);
-}
 
 template <int D, int BLK, Share SHARE>
 __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_waves(D, BLK), dq_waves(D, BLK)))) void psa_mapped_dq_kernel(MapArgs a) {
@@ -1088,37 +1111,53 @@ int32_t map_parts(int32_t n_bh, int32_t nbq, int32_t nbk, int32_t block) {
   return (int32_t)std::max<int64_t>(1, std::min<int64_t>(room / items, nbk / 6));
 }
 
-MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
-  MapLayout l = {};
-  l.parts = map_parts(n_bh, nbq, nbk, block);
-  const size_t items = (size_t)n_bh * nbq, rows = items * l.parts * block;
-  if (l.parts > 1) {
-    l.part_ml = up256(rows * head_dim * sizeof(float));
-    l.total = l.part_ml + up256(rows * sizeof(float2));
-  } else if (ordered(items, block)) {
-    const size_t pairs = up256((size_t)n_bh * pairs_per_head(nbq) * sizeof(int32_t));
-    l.row_order = up256(items * sizeof(int32_t));
-    l.pair_counts = 2 * l.row_order;
-    l.pair_order = l.pair_counts + pairs;
-    l.paired = l.pair_order + pairs;
-    l.total = l.paired + 256;
-  }
-  return l;
-}
-
-// The order of a backward kernel's `items`, whose lists hold at most `longest` blocks and would else go in `parts` each.
-// Items that all run at once are ordered too if a part may last long: the order costs 10 to 20 us of a balanced call, a
-// block of 64 takes 1.2 us and one of 128 2.4.  (D 128, blocks of 64, equal parts and the order, in us: 4 heads over 2 x 7791
+// The order of a kernel's `items`, whose lists hold at most `longest` blocks and would else go in `parts` each.  Items that
+// all run at once are ordered too if a part may hold more than a kernel's `long_part` tokens: the order costs 10 to
+// 20 us of a balanced call, a block of 128 2.4 us in the gradients' kernels and 1 us in the forward's, one of 64
+// half as much.  (Gradients, D 128, blocks of 64, equal parts and the order, in us: 4 heads over 2 x 7791
 // with 226 of text, 31 kept, 337 and 230; without text 4 over 2 x 5760, 43 kept, 171 and 189; 3 heads x 2430 in a batch of
 // 4, whose lists stay below, 130 and 160.)
-Pieces pieces_for(int64_t items, int64_t longest, int32_t parts, int32_t block) {
+Pieces pieces_for(int64_t items, int64_t longest, int32_t parts, int32_t long_part, int32_t block) {
   Pieces p = {};
   const int64_t room = room_of(block);
-  if (!ordered(items, block) && longest / parts * block <= 24 * 128) return p;
+  if (!ordered(items, block) && longest / parts * block <= long_part) return p;
   p.pieces = (int32_t)std::min(3 * room, items * ((longest + kFewBlocks - 1) / kFewBlocks));
   p.splits = (int32_t)std::min(room, items);
   p.grid = (int32_t)(items + p.pieces);
   return p;
+}
+
+constexpr int32_t kLongForward = 8000, kLongBackward = 3000;
+// No forward list shorter than this goes in pieces: they cost a launch more, 5 us (20 heads x 2400 in a batch of 2, 226 of
+// text, blocks of 64: 86 and 90 us; 8 x 4096: 65 and 63; 4 x 8192: 119 and 66; 3 x 16384: 235 and 105).
+constexpr int32_t kShortForward = 6000;
+
+MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
+  MapLayout l = {};
+  l.parts = map_parts(n_bh, nbq, nbk, block);
+  // (single query blocks that all run at once: a few tokens behind a cache, lists as long as each other)
+  const int64_t items = (int64_t)n_bh * nbq;
+  if (nbq > 1 || ordered(items, block)) l.rows = pieces_for(items, nbk, l.parts, kLongForward, block);
+  auto take = [&](size_t& at, size_t bytes) {
+    at = l.total;
+    l.total += up256(bytes);
+  };
+  if (l.rows.grid) {
+    l.parts = 1;
+    if ((int64_t)nbk * block < kShortForward) l.rows.pieces = l.rows.splits = 0, l.rows.grid = (int32_t)items;
+    take(l.row_counts, (size_t)n_bh * nbq * sizeof(int32_t));
+    take(l.row_order, l.rows.grid * sizeof(int2));
+    take(l.row_split, (1 + (size_t)l.rows.splits) * sizeof(int4));
+    if (block == 64 && ordered(items, block)) {
+      take(l.pair_counts, (size_t)n_bh * pairs_per_head(nbq) * sizeof(int32_t));
+      take(l.pair_order, (size_t)n_bh * pairs_per_head(nbq) * sizeof(int32_t));
+      take(l.paired, sizeof(int32_t));
+    }
+  }
+  const size_t tiles = l.rows.grid ? l.rows.pieces : l.parts > 1 ? (size_t)n_bh * nbq * l.parts : 0;
+  take(l.part_o, tiles * block * head_dim * sizeof(float));
+  take(l.part_ml, tiles * block * sizeof(float2));
+  return l;
 }
 
 MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
@@ -1129,8 +1168,8 @@ MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_
   l.head_parts = std::min(group, room);
   l.list_parts = std::max(1, std::min(room / l.head_parts, nbq / 6));
   const int32_t kv_parts = l.head_parts * l.list_parts;
-  l.rows = pieces_for((int64_t)n_bh * nbq, nbk, l.parts, block);
-  l.cols = pieces_for((int64_t)n_kv * nbk, (int64_t)group * nbq, kv_parts, block);
+  l.rows = pieces_for((int64_t)n_bh * nbq, nbk, l.parts, kLongBackward, block);
+  l.cols = pieces_for((int64_t)n_kv * nbk, (int64_t)group * nbq, kv_parts, kLongBackward, block);
   const size_t tile = (size_t)block * head_dim * sizeof(float);
   auto take = [&](size_t& at, size_t bytes) {
     at = l.total;
@@ -1170,37 +1209,44 @@ static hipError_t launch_prepare(const MapArgs& a, bool backward, hipStream_t st
                      row_groups);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || (!a.row_counts && !a.col_counts)) return e;
-  const Order row = backward ? Order::kRowPieces : Order::kRows, other = backward ? Order::kColPieces : Order::kPairs;
+  const Order other = backward ? Order::kCols : Order::kPairs;
   const bool both = a.row_counts && (backward ? a.col_counts != nullptr : a.paired != nullptr);
   hipLaunchKernelGGL(psa_mapped_order_kernel, dim3(both ? 2 : 1), dim3(kOrderThreads), 0, stream, a,
-                     a.row_counts ? row : other, other, D, room_of(a.block));
+                     a.row_counts ? Order::kRows : other, other, D, room_of(a.block));
   return hipGetLastError();
 }
 
 hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream) {
   return by_shape(head_dim, a.block, [&](auto dim, auto blk) {
     constexpr int D = decltype(dim)::value, B = decltype(blk)::value;
+    constexpr int kLanes = D / 4, kSide = 256 / kLanes;
+    const int32_t items = a.n_bh * a.nbq, rows = a.n_bh * a.n_q, list = list_bytes(a.nbk);
+    const dim3 threads(4 * B);
     hipError_t e = launch_prepare<D>(a, false, stream);
     if (e != hipSuccess) return e;
-    const dim3 grid(a.n_bh * a.nbq * a.parts);
-    if (a.parts == 1) {
-      if constexpr (B == 64) {
-        if (a.paired)
-          hipLaunchKernelGGL((psa_mapped_pairs_kernel<D>), dim3(a.n_bh * pairs_per_head(a.nbq)), dim3(256),
-                             list_bytes(a.nbk), stream, a);
+    if (a.row_pieces.grid) {
+      if (B == 64 && a.paired) {
+        hipLaunchKernelGGL((psa_mapped_pairs_kernel<D>), dim3(a.n_bh * pairs_per_head(a.nbq)), dim3(256), list, stream, a);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
       }
-      hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, false>), grid, dim3(4 * B), list_bytes(a.nbk), stream, a);
-      return hipGetLastError();
+      hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, Share::kOrder>), dim3(a.row_pieces.grid), threads, list, stream, a);
+      e = hipGetLastError();
+      if (e != hipSuccess || a.row_pieces.splits == 0) return e;
+      hipLaunchKernelGGL((psa_mapped_join_kernel<D, B, Share::kOrder, 1>), dim3(a.row_pieces.splits, B / kSide), dim3(256), 0,
+                         stream, a);
+    } else if (a.parts == 1) {
+      hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, Share::kWhole>), dim3(items), threads, list, stream, a);
+    } else {
+      hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, Share::kParts>), dim3(items * a.parts), threads, list, stream, a);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      if (a.parts <= 4)
+        hipLaunchKernelGGL((psa_mapped_join_kernel<D, B, Share::kParts, 1>), dim3((rows + kSide - 1) / kSide), dim3(256), 0,
+                           stream, a);
+      else
+        hipLaunchKernelGGL((psa_mapped_join_kernel<D, B, Share::kParts, kSide>), dim3(rows), dim3(256), 0, stream, a);
     }
-    hipLaunchKernelGGL((psa_mapped_fwd_kernel<D, B, true>), grid, dim3(4 * B), list_bytes(a.nbk), stream, a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    constexpr int kLanes = D / 4, kSide = 256 / kLanes;
-    const int32_t rows = a.n_bh * a.n_q;
-    if (a.parts <= 4)
-      hipLaunchKernelGGL((psa_mapped_join_kernel<D, B, 1>), dim3((rows + kSide - 1) / kSide), dim3(256), 0, stream, a);
-    else
-      hipLaunchKernelGGL((psa_mapped_join_kernel<D, B, kSide>), dim3(rows), dim3(256), 0, stream, a);
     return hipGetLastError();
   });
 }

@@ -115,7 +115,7 @@ def check_backward(q, k, v, do, m, block, scale, o, lse, got, heads, pool=True):
     assert not pool or num <= gu.REL_L2_TOL ** 2 * den
 
 
-def check(b, h, hk, n_q, n_k, block, d, density=0.4, scale=None, heads=None, seed=0, m=None, data=None, pool=True):
+def check(b, h, hk, n_q, n_k, block, d, density=0.4, scale=None, heads=None, seed=0, m=None, data=None, pool=True, backward=True):
     torch = gu.torch()
     print(b, h, hk, n_q, n_k, block, d, density, flush=True)
     q, k, v, do = inputs(seed, b, h, hk, n_q, n_k, d) if data is None else data
@@ -128,6 +128,8 @@ def check(b, h, hk, n_q, n_k, block, d, density=0.4, scale=None, heads=None, see
     heads = range(h) if heads is None else heads
     on, ln = bits(o), lse.cpu().numpy()
     check_forward(q, k, v, m, block, s, on, ln, heads)
+    if not backward:
+        return
     got = psa.attention_map_bwd(t[3], t[0], t[1], t[2], o, lse, dm, block, scale)
     torch.cuda.synchronize()
     check_backward(q, k, v, do, m, block, s, on, ln, got, heads, pool)
@@ -186,6 +188,13 @@ def test_few_long_lists_of_other_lengths(d, block, hk, density):
     """As many query and key blocks as run at once and fewer: a row and a column kept whole go in pieces."""
     n = (56 if block == 64 else 31) * block
     check(1, 8, hk, n - 9, n - 1, block, d, density=density, heads=[0, 7])
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
+@pytest.mark.parametrize("h,hk,n_k,density", [(8, 4, 6150, 0.05), (4, 4, 8190, 0.1), (8, 1, 7000, 0.0), (8, 8, 6150, 0.95)])
+def test_long_rows_among_short_ones(d, block, h, hk, n_k, density):
+    """Rows kept whole of many and of few query blocks go in pieces, where these are longer than the others by far."""
+    check(1, h, hk, 66 * 64 - 11, n_k, block, d, density=density, heads=[0, h - 1], backward=False)
 
 
 @pytest.mark.parametrize("d,block", SHAPES)
