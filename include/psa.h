@@ -414,7 +414,8 @@ psa_status_t psa_select_blocks(const void* q, const psa_kv_t* kv, int32_t batch,
 
 /* Bytes of device workspace of psa_attention_map_fwd (0 if invalid, or if none is needed).  Calls of few query
  * blocks, whose lists are shared out over several workgroups, keep their partial sums there, calls of many the
- * order in which they are taken, those with the longest lists first. */
+ * order in which they are taken and partial sums of the longest lists: at most about 50 MB and 20 bytes for every
+ * (head, query block). */
 size_t psa_attention_map_workspace_size(int32_t batch, int32_t n_heads, int32_t head_dim, int32_t n_q,
                                         int32_t n_k, int32_t block);
 
@@ -425,6 +426,8 @@ size_t psa_attention_map_workspace_size(int32_t batch, int32_t n_heads, int32_t 
  *                (0: the same map for all)
  *   lse          device fp32 [batch][n_heads][n_q], or NULL
  *   workspace    device, psa_attention_map_workspace_size() bytes, 256-byte aligned (NULL if 0)
+ * o and lse must not overlap an input.  Every batch element has all n_q and n_k tokens: of a padded batch, clear the
+ * map's bytes of the blocks that are padding alone, and let the sequences end in whole blocks.
  * head_dim and block 64 or 128; at most PSA_MAX_BLOCKS blocks on each side. */
 psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, int32_t batch,
                                    int32_t n_heads, int32_t head_dim, int32_t n_q, int32_t n_k,
@@ -432,7 +435,8 @@ psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, i
                                    float softmax_scale, float* lse, void* workspace,
                                    size_t workspace_bytes, hipStream_t stream);
 
-/* Bytes of device workspace of psa_attention_map_bwd (0 if invalid). */
+/* Bytes of device workspace of psa_attention_map_bwd (0 if invalid): at most about 150 MB, 8 bytes for every (head, query)
+ * and 12 for every (head, block). */
 size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads,
                                             int32_t head_dim, int32_t n_q, int32_t n_k, int32_t block);
 

@@ -789,7 +789,7 @@ __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
 // ---------------------------------------------------------------------------------------------
 
 // Waves per SIMD of dq's kernel: at head dim 64 the registers allow more than two, and no unit alone bounds it (12 heads
-// x 16000, dq, dk and dv: block 64 784 us with two, 761 with three, 783 with four; block 128 761, 759, 740).
+// x 16000, a fifth kept, dq, dk and dv: block 64 659 us with two, 639 with three, 660 with four; block 128 641, 635, 630).
 constexpr int dq_waves(int d, int blk) { return d == 128 ? 2 : blk == 64 ? 3 : 4; }
 
 template <int D, int BLK, Share SHARE>

