@@ -78,17 +78,17 @@ __device__ __forceinline__ int32_t item_of(int32_t blk, int32_t items) {
   return blk >= part * kNumQueues ? blk : blk % kNumQueues * part + blk / kNumQueues;
 }
 
-// Whether maps of 64 run on pairs of query blocks: `either` counts the key blocks that one block of a pair or both keep,
-// `single` those that each keeps, over all pairs.  A wave waits while its neighbour's block alone is worked on, so
-// pairs pay where neighbours share enough; at head dim 64, whose four waves per SIMD cover such waits, in long lists
-// always.  Microseconds in pairs and one by one at either / single 0.88, 0.71 and 0.50:
-//   head dim 64   12 heads x 32760, density 0.25 (256 pairs each)  1102, 963, 861 and 1259, 1191, 1190
-//                 8 x 8000, 0.2 (63 pairs each)                81, 71, 58     and 69, 70, 70
-//   head dim 128  12 x 32760, 0.25                             2039, 1779, 1540 and 1840, 1820, 1822
-//                 8 x 8000, 0.2                                105, 88, 78    and 94, 94, 92
-constexpr int32_t kManyPairs = 2048;        // twice the workgroups that run at once
-__device__ __forceinline__ bool pairs_pay(unsigned long long either, unsigned long long single, int32_t pairs, int32_t head_dim) {
-  return head_dim == 64 ? pairs >= kManyPairs || either * 100 <= single * 73 : either * 10 <= single * 7;
+// Whether maps of 64 run on pairs of query blocks, where these outnumber the workgroups: `either` counts the key blocks
+// that one block of a pair or both keep, `single` those that each keeps, over all pairs.  A wave waits while its
+// neighbour's block alone is worked on, so at head dim 128 pairs pay where neighbours share enough; at head dim 64 its
+// four waves per SIMD cover such waits.  Microseconds in pairs and one by one at either / single 0.87, 0.70 and 0.50:
+//   head dim 64   12 heads x 32760, density 0.25 (256 pairs each)  1104, 1009, 895 and 1281, 1284, 1288
+//                 16 x 8000, 0.2 (63 pairs each)                   107, 94, 85     and 118, 118, 116
+//                 9 x 8000, 0.2                                    90, 81, 67      and 91, 88, 87
+//   head dim 128  12 x 32760, 0.25                                 2129, 1923, 1645 and 2046, 2006, 1962
+//                 8 x 8000, 0.2                                    110, 96, 83     and 97, 95, 91
+__device__ __forceinline__ bool pairs_pay(unsigned long long either, unsigned long long single, int32_t head_dim) {
+  return head_dim == 64 || either * 10 <= single * 7;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -377,7 +377,7 @@ __device__ __forceinline__ void order_pairs(const MapArgs& a, int32_t head_dim, 
   int32_t any = 0;
   rows.each([&](int32_t, int32_t c) { any |= cut.cuts(c); });
   any = __syncthreads_or(any);
-  if (threadIdx.x == 0) *a.paired = !any && pairs_pay(either, single, items.n, head_dim) ? 1 : 0;
+  if (threadIdx.x == 0) *a.paired = !any && pairs_pay(either, single, head_dim) ? 1 : 0;
   const float mean = (float)either / (float)items.n;
   place_items(items, s.at, s.waves, [&](int32_t c) { return length_class(c, mean); },
               [&](int32_t i, int32_t place) { a.pair_order[place] = i; });
@@ -791,6 +791,9 @@ __global__ __launch_bounds__(256) void psa_mapped_join_kernel(MapArgs a) {
 // Waves per SIMD of dq's kernel: at head dim 64 the registers allow more than two, and no unit alone bounds it (12 heads
 // x 16000, a fifth kept, dq, dk and dv: block 64 659 us with two, 639 with three, 660 with four; block 128 641, 635, 630).
 constexpr int dq_waves(int d, int blk) { return d == 128 ? 2 : blk == 64 ? 3 : 4; }
+// ... of dk's and dv's: head dim 64 and block 64 have room for a third wave (12 heads x 16000, a fifth kept, all three
+// gradients: 625 us with two, 592 with three); elsewhere another workgroup would need half the registers.
+constexpr int dkv_waves(int d, int blk) { return d == 64 && blk == 64 ? 3 : 2; }
 
 template <int D, int BLK, Share SHARE>
 __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_waves(D, BLK), dq_waves(D, BLK)))) void psa_mapped_dq_kernel(MapArgs a) {
@@ -910,7 +913,7 @@ __global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dq_wave
 }
 
 template <int D, int BLK, Share SHARE>
-__global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(2, 2))) void psa_mapped_dkv_kernel(MapArgs a) {
+__global__ __launch_bounds__(BLK * 4) __attribute__((amdgpu_waves_per_eu(dkv_waves(D, BLK), dkv_waves(D, BLK)))) void psa_mapped_dkv_kernel(MapArgs a) {
   using T = Tile<D, BLK>;
   constexpr int HQ = BLK / 2, W = 2 * T::kWaves;
   __shared__ __attribute__((aligned(1024))) uint8_t sq[2][T::BYTES];
@@ -1085,9 +1088,11 @@ __global__ __launch_bounds__(256) void psa_mapped_sum_kernel(AllSums all) {
       *(bf16x4*)(dst + 4 * (at + 256 * u)) = __builtin_convertvector(s[u] * p.scale, bf16x4);
 }
 
-// Whether the items are more than the workgroups that run at once (one of 128 rows to a CU, two of 64).
+// Workgroups that share a call's work: one of 128 rows to a CU, two of 64.
 int32_t room_of(int32_t block) { return 256 * (128 / block); }
-bool ordered(int64_t items, int32_t block) { return items > room_of(block); }
+// Forward items that run at once, twice as many at head dim 64.  No more than these are not ordered: ordered and not, 8
+// heads x 5000 take 36 and 24 us at block 64, 44 and 36 at block 128; 8 x 8000 at block 64 67 and 52.
+int32_t at_once(int32_t head_dim, int32_t block) { return room_of(block) * (128 / head_dim); }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -1112,15 +1117,15 @@ int32_t map_parts(int32_t n_bh, int32_t nbq, int32_t nbk, int32_t block) {
 }
 
 // The order of a kernel's `items`, whose lists hold at most `longest` blocks and would else go in `parts` each.  Items that
-// all run at once are ordered too if a part may hold more than a kernel's `long_part` tokens: the order costs 10 to
+// all run at once (`at_once` of them) are ordered too if a part may hold more than a kernel's `long_part` tokens: the order costs 10 to
 // 20 us of a balanced call, a block of 128 2.4 us in the gradients' kernels and 1 us in the forward's, one of 64
 // half as much.  (Gradients, D 128, blocks of 64, equal parts and the order, in us: 4 heads over 2 x 7791
 // with 226 of text, 31 kept, 337 and 230; without text 4 over 2 x 5760, 43 kept, 171 and 189; 3 heads x 2430 in a batch of
 // 4, whose lists stay below, 130 and 160.)
-Pieces pieces_for(int64_t items, int64_t longest, int32_t parts, int32_t long_part, int32_t block) {
+Pieces pieces_for(int64_t items, int32_t at_once, int64_t longest, int32_t parts, int32_t long_part, int32_t block) {
   Pieces p = {};
   const int64_t room = room_of(block);
-  if (!ordered(items, block) && longest / parts * block <= long_part) return p;
+  if (items <= at_once && longest / parts * block <= long_part) return p;
   p.pieces = (int32_t)std::min(3 * room, items * ((longest + kFewBlocks - 1) / kFewBlocks));
   p.splits = (int32_t)std::min(room, items);
   p.grid = (int32_t)(items + p.pieces);
@@ -1137,7 +1142,8 @@ MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, i
   l.parts = map_parts(n_bh, nbq, nbk, block);
   // (single query blocks that all run at once: a few tokens behind a cache, lists as long as each other)
   const int64_t items = (int64_t)n_bh * nbq;
-  if (nbq > 1 || ordered(items, block)) l.rows = pieces_for(items, nbk, l.parts, kLongForward, block);
+  const int32_t slots = at_once(head_dim, block);
+  if (nbq > 1 || items > slots) l.rows = pieces_for(items, slots, nbk, l.parts, kLongForward, block);
   auto take = [&](size_t& at, size_t bytes) {
     at = l.total;
     l.total += up256(bytes);
@@ -1148,7 +1154,7 @@ MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, i
     take(l.row_counts, (size_t)n_bh * nbq * sizeof(int32_t));
     take(l.row_order, l.rows.grid * sizeof(int2));
     take(l.row_split, (1 + (size_t)l.rows.splits) * sizeof(int4));
-    if (block == 64 && ordered(items, block)) {
+    if (block == 64 && items > slots) {
       take(l.pair_counts, (size_t)n_bh * pairs_per_head(nbq) * sizeof(int32_t));
       take(l.pair_order, (size_t)n_bh * pairs_per_head(nbq) * sizeof(int32_t));
       take(l.paired, sizeof(int32_t));
@@ -1168,8 +1174,8 @@ MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_
   l.head_parts = std::min(group, room);
   l.list_parts = std::max(1, std::min(room / l.head_parts, nbq / 6));
   const int32_t kv_parts = l.head_parts * l.list_parts;
-  l.rows = pieces_for((int64_t)n_bh * nbq, nbk, l.parts, kLongBackward, block);
-  l.cols = pieces_for((int64_t)n_kv * nbk, (int64_t)group * nbq, kv_parts, kLongBackward, block);
+  l.rows = pieces_for((int64_t)n_bh * nbq, room_of(block), nbk, l.parts, kLongBackward, block);
+  l.cols = pieces_for((int64_t)n_kv * nbk, room_of(block), (int64_t)group * nbq, kv_parts, kLongBackward, block);
   const size_t tile = (size_t)block * head_dim * sizeof(float);
   auto take = [&](size_t& at, size_t bytes) {
     at = l.total;

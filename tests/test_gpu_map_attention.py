@@ -191,7 +191,7 @@ def test_few_long_lists_of_other_lengths(d, block, hk, density):
 
 
 @pytest.mark.parametrize("d,block", SHAPES)
-@pytest.mark.parametrize("h,hk,n_k,density", [(8, 4, 6150, 0.05), (4, 4, 8190, 0.1), (8, 1, 7000, 0.0), (8, 8, 6150, 0.95)])
+@pytest.mark.parametrize("h,hk,n_k,density", [(8, 4, 6150, 0.05), (16, 8, 6150, 0.05), (4, 4, 8190, 0.1), (8, 1, 7000, 0.0), (8, 8, 6150, 0.95)])
 def test_long_rows_among_short_ones(d, block, h, hk, n_k, density):
     """Rows kept whole of many and of few query blocks go in pieces, where these are longer than the others by far."""
     check(1, h, hk, 66 * 64 - 11, n_k, block, d, density=density, heads=[0, h - 1], backward=False)
