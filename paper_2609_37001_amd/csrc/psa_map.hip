@@ -185,9 +185,7 @@ __global__ __launch_bounds__(256) void psa_mapped_prepare_kernel(MapArgs a, int3
   }
 }
 
-constexpr int kOrderThreads = 1024, kOrderClasses = 8, kOrderRun = 8;
-
-constexpr int kOrderWaves = kOrderThreads / 64;
+constexpr int kOrderThreads = 1024, kOrderWaves = kOrderThreads / 64, kOrderClasses = 8, kOrderRun = 8;
 
 struct OrderSpace {
   int32_t at[kOrderClasses * kOrderThreads * 33 / 32], waves[kOrderWaves];
@@ -337,7 +335,7 @@ struct Cut {
     up = few ? 0.5f : 1.0f;
   }
   __device__ __forceinline__ bool cuts(int32_t c) const { return (float)c > longest; }
-  __device__ __forceinline__ int32_t pieces(int32_t c) const { return (int32_t)((float)c / piece + up); }     // of one that it cuts
+  __device__ __forceinline__ int32_t pieces(int32_t c) const { return (int32_t)((float)c / piece + up); }   // of such a list
 };
 
 //   order[workgroup] = (item, piece << 16 | pieces): the pieces first, then the whole items by their lengths, then -1
@@ -1117,11 +1115,12 @@ int32_t map_parts(int32_t n_bh, int32_t nbq, int32_t nbk, int32_t block) {
 }
 
 // The order of a kernel's `items`, whose lists hold at most `longest` blocks and would else go in `parts` each.  Items that
-// all run at once (`at_once` of them) are ordered too if a part may hold more than a kernel's `long_part` tokens: the order costs 10 to
-// 20 us of a balanced call, a block of 128 2.4 us in the gradients' kernels and 1 us in the forward's, one of 64
-// half as much.  (Gradients, D 128, blocks of 64, equal parts and the order, in us: 4 heads over 2 x 7791
-// with 226 of text, 31 kept, 337 and 230; without text 4 over 2 x 5760, 43 kept, 171 and 189; 3 heads x 2430 in a batch of
-// 4, whose lists stay below, 130 and 160.)
+// all run at once (`at_once` of them) are ordered too if a part may hold more than a kernel's `long_part` tokens: the
+// order costs 10 to 20 us of a balanced call, a block of 128 takes 2.4 us in the gradients' kernels and 1 us in the
+// forward's, one of 64 half as much.  (Gradients, D 128, blocks of 64, equal parts and the order, in us: 4 heads over 2 x
+// 7791 with 226 of text, 31 kept, 337 and 228; without text 4 over 2 x 5760, 43 kept, 171 and 187; 3 heads x 2430 in a
+// batch of 4, whose lists stay below, 130 and 160.  Forward: 4 x 8192 with text, 16 kept, 119 and 66; 2 x 16384
+// without, 40 kept, 63 and 67.)
 Pieces pieces_for(int64_t items, int32_t at_once, int64_t longest, int32_t parts, int32_t long_part, int32_t block) {
   Pieces p = {};
   const int64_t room = room_of(block);
