@@ -338,7 +338,8 @@ struct Cut {
   __device__ __forceinline__ int32_t pieces(int32_t c) const { return (int32_t)((float)c / piece + up); }   // of such a list
 };
 
-//   order[workgroup] = (item, piece << 16 | pieces): the pieces first, then the whole items by their lengths, then -1
+//   order[workgroup] = (item, piece << 16 | pieces): the pieces first (a piece's tile of the workspace is its workgroup's
+//                      number), then the whole items by their lengths, then -1
 //   split[i]         = (item, workgroup of its first piece, pieces), split[-1].x their number
 __device__ __forceinline__ void order_pieces(const Items& items, const Pieces& to, int32_t room, OrderSpace& s) {
   const Cut cut(items.sum(s.totals), items.n, room, to);
