@@ -463,3 +463,34 @@ def test_together_on_a_side_stream_and_in_a_graph():
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
+@pytest.mark.parametrize("d,block,h,hk,n", [(128, 128, 8, 4, 6200), (64, 64, 16, 16, 6200), (128, 64, 4, 2, 8100)])
+def test_replays_over_other_maps(d, block, h, hk, n):
+    """A captured call orders and cuts the lists of the map that a replay finds: long rows and columns, none, all."""
+    torch = gu.torch()
+    q, k, v, do = (torch.randn(1, m, n, d, device="cuda:0").bfloat16() for m in (h, hk, hk, h))
+    nb = blocks(n, block)
+    bm = torch.zeros(1, h, nb, nb, dtype=torch.uint8, device="cuda:0")
+
+    def layer():
+        o, lse = psa.attention_map_fwd(q, k, v, bm, block, return_lse=True)
+        return (o, lse) + psa.attention_map_bwd(do, q, k, v, o, lse, bm, block)
+
+    layer()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = layer()
+    for seed, density in ((61, 0.1), (62, 0.0), (63, 0.5), (64, 1.0), (61, 0.1)):
+        m = np.ones((1, h, nb, nb), np.uint8) if density == 1.0 else random_map(seed, 1, h, nb, nb, density)
+        bm.copy_(torch.from_numpy(m))
+        ref = layer()
+        for t in got:
+            t.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    check_forward(bits(q), bits(k), bits(v), m, block, d ** -0.5, bits(got[0]), got[1].cpu().numpy(), [h - 1])
+    check_backward(bits(q), bits(k), bits(v), bits(do), m, block, d ** -0.5, bits(got[0]), got[1].cpu().numpy(), got[2:], [h - 1])
