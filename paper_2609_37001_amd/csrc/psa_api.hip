@@ -277,13 +277,21 @@ psa_status_t check_rows(const psa_rows_t& r, const char* what, int32_t batch, in
   return PSA_OK;
 }
 
+// Bytes of partial sums of a backward with a norm; `a` holds checked sizes and heads.
+size_t rope_partial_bytes(const psa::RopeArgs& a, int32_t head_dim) {
+  return (size_t)(psa::rope_partial_rows(a, head_dim) * a.n_tensors * head_dim) * sizeof(float);
+}
+
+// Whether a launch can number the batch elements of all its tensors.
+bool rope_batch_fits(int32_t batch, int32_t n_tensors) { return (int64_t)batch * n_tensors <= 65535; }
+
 // Shapes and the rotation of a norm-and-rotation call; fills all of `a` but its tensors.
 psa_status_t check_rope(int32_t type, int32_t batch, int32_t n_tensors, int32_t head_dim, const psa_rope_t* rope,
                         int32_t norm, const float* q_weight, const float* k_weight, float eps, psa::RopeArgs* a) {
   if (type != PSA_TYPE_BF16 && type != PSA_TYPE_FP32)
     return fail(PSA_ERR_UNSUPPORTED, "type must be PSA_TYPE_BF16 or PSA_TYPE_FP32 (got %d)", type);
   if (batch < 1) return fail(PSA_ERR_INVALID, "batch must be >= 1 (got %d)", batch);
-  if ((int64_t)batch * n_tensors > 65535) return fail(PSA_ERR_UNSUPPORTED, "batch %d is too large", batch);
+  if (!rope_batch_fits(batch, n_tensors)) return fail(PSA_ERR_UNSUPPORTED, "batch %d is too large", batch);
   if (head_dim != 64 && head_dim != 128)
     return fail(PSA_ERR_UNSUPPORTED, "head_dim must be 64 or 128 (got %d)", head_dim);
   if (!rope) return fail(PSA_ERR_INVALID, "rope is NULL");
@@ -698,16 +706,17 @@ psa_status_t psa_qk_norm_rope_fwd(const psa_rows_t* q, const psa_rows_t* k, void
 size_t psa_qk_norm_rope_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads,
                                        int32_t head_dim, psa_grid_t grid, int32_t norm) {
   psa::Geometry g;
+  const int32_t n_tensors = n_kv_heads > 0 ? 2 : 1;
   if (!norm || batch < 1 || n_heads < 1 || n_kv_heads < 0 || (head_dim != 64 && head_dim != 128) ||
-      (int64_t)batch * 2 > 65535 || !grid_geometry(grid, 1, &g))
+      !rope_batch_fits(batch, n_tensors) || !grid_geometry(grid, 1, &g))
     return 0;
   psa::RopeArgs a = {};
   a.batch = batch;
   a.n = g.n;
-  a.n_tensors = n_kv_heads > 0 ? 2 : 1;
+  a.n_tensors = n_tensors;
   a.t[0].n_heads = n_heads;
   a.t[1].n_heads = n_kv_heads;
-  return (size_t)(psa::rope_partial_rows(a, head_dim) * a.n_tensors * head_dim) * sizeof(float);
+  return rope_partial_bytes(a, head_dim);
 }
 
 psa_status_t psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const psa_rows_t* q,
@@ -743,7 +752,7 @@ psa_status_t psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const 
     a.t[i].dx_stride_h = grads[i]->stride_h;
     a.t[i].dx_stride_n = grads[i]->stride_n;
   }
-  const size_t need = psa_qk_norm_rope_workspace_size(batch, q->n_heads, k ? k->n_heads : 0, head_dim, rope->grid, norm);
+  const size_t need = norm ? rope_partial_bytes(a, head_dim) : 0;
   if (norm && (!workspace || workspace_bytes < need))
     return fail(PSA_ERR_WORKSPACE, "workspace of %zu bytes at %p; %zu bytes required", workspace_bytes, workspace, need);
   if (!aligned(workspace, 256)) return fail(PSA_ERR_WORKSPACE, "workspace must be 256-byte aligned");

@@ -210,3 +210,31 @@ def test_side_stream_and_graph_replays_match_eager():
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got + gg, out + grads))
+
+
+def test_queries_alone_in_a_large_batch():
+    """More batch elements than queries and keys together may have, in a workspace of exactly the size asked for."""
+    torch = gu.torch()
+    from paper_2609_37001_amd import _lib
+    b, grid, d = 40000, (1, 1, 3, 0), 64
+    q = torch.randn(b, 1, 3, d, device="cuda:0").bfloat16()
+    dy = torch.randn_like(q)
+    w = 1 + 0.2 * torch.randn(d, device="cuda:0")
+    need = _lib.lib().psa_qk_norm_rope_workspace_size(b, 1, 0, d, _lib.grid_of(*grid), 1)
+    room = torch.full((need + 4096,), 7, dtype=torch.uint8, device="cuda:0")
+    y = psa.qk_norm_rope(q, None, grid, AXES[d], q_weight=w)[0]
+    dq, _, dw, _ = psa.qk_norm_rope_bwd(dy, None, q, None, grid, AXES[d], q_weight=w, workspace=room[:need])
+    own = psa.qk_norm_rope_bwd(dy, None, q, None, grid, AXES[d], q_weight=w)
+    torch.cuda.synchronize()
+    assert (room[need:] == 7).all() and torch.equal(own[0], dq) and torch.equal(own[2], dw)
+    xn, dyn, wn = (t.double().cpu().numpy() for t in (q, dy, w))
+    ang = rope.angles(grid, AXES[d], head_dim=d)
+    ref = rope.norm_rope(xn, ang, wn)
+    near(y, ref, np.abs(ref).max(-1, keepdims=True) * 2 ** 0.5, 2.0 ** -8)
+    dx, dref = rope.norm_rope_grad(dyn, xn, ang, wn)
+    r = 1 / np.sqrt((xn * xn).mean(-1, keepdims=True) + 1e-6)
+    g, u = rope.rotate(dyn, -ang), np.abs(xn * r)
+    gw = np.abs(g * wn)
+    near(dq, dx, r * (gw.max(-1, keepdims=True) + u.max(-1, keepdims=True) * (gw * u).mean(-1, keepdims=True)), 2.0 ** -8)
+    terms = np.abs(g * xn * r).reshape(-1, d).sum(0)
+    assert (np.abs(dw.double().cpu().numpy() - dref) <= 2.0 ** -16 * terms + 2.0 ** -24 * np.abs(dref)).all()

@@ -125,3 +125,17 @@ def test_workspace_sizes():
     assert L.psa_attention_map_workspace_size(1, 4, 100, 1, 75600, 128) == 0
     assert L.psa_attention_map_bwd_workspace_size(2, 3, 1, 64, 65, 99, 64) >= 2 * 4 * 2 * 3 * 128
     assert L.psa_attention_map_bwd_workspace_size(2, 3, 3, 64, 65, 99, 32) == 0
+
+
+@pytest.mark.parametrize("batch", [32767, 32768, 65535])
+def test_norm_rope_workspace_of_queries_alone_up_to_the_largest_batch(batch):
+    """batch * tensors may reach 65535: without keys every such batch has a workspace, and no smaller one passes."""
+    L, d = _lib.lib(), 64
+    need = L.psa_qk_norm_rope_workspace_size(batch, 1, 0, d, _lib.grid_of(1, 2, 3, 1), 1)
+    assert need >= 4 * d * batch                               # a row of partial sums of each batch element at least
+    x = rows(heads=1)
+    for ws, nbytes in ((256, 256), (256, need - 1), (0, 0)):
+        assert L.psa_qk_norm_rope_bwd(vp(256), None, x, None, x, None, vp(256), None, 0, batch, d, rope(), 1, None, None,
+                                      1e-6, vp(ws), nbytes, None) == WORKSPACE
+    assert L.psa_qk_norm_rope_workspace_size(65536, 1, 0, d, _lib.grid_of(1, 2, 3, 1), 1) == 0
+    assert L.psa_qk_norm_rope_workspace_size(32768, 1, 1, d, _lib.grid_of(1, 2, 3, 1), 1) == 0
