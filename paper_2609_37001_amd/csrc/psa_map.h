@@ -3,6 +3,7 @@
 #pragma once
 
 #include "psa_launch.h"
+#include "psa_pieces.h"
 
 namespace psa {
 
@@ -24,13 +25,6 @@ SelectLayout select_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t
 hipError_t launch_select(const SelectArgs& args, int32_t head_dim, hipStream_t stream);
 
 // Attention over a block map.
-// Order of a kernel's items (psa_map.hip, order_pieces): `grid` workgroups (0: there is none), of which at most
-// `pieces` (0: the lists stay whole) take a piece of a list, of at most `splits` items.
-struct Pieces {
-  int2* order;
-  int4* split;
-  int32_t grid, pieces, splits;
-};
 struct MapArgs {
   const __bf16 *q, *k, *v;            // q [n_bh][n_q][d]; k and v by strides, rows contiguous
   const __bf16* grad_o;               // backward
@@ -54,19 +48,7 @@ struct MapArgs {
   float c, scale;                     // scale log2(e), scale
   float pow2, factor;                 // forward: c = pow2 factor, a power of two with c's sign and a factor in [1, 2)
 };
-struct MapLayout {
-  Pieces rows;                        // sizes alone
-  int32_t parts;
-  size_t row_counts, row_order, row_split, pair_counts, pair_order, paired, part_o, part_ml, total;
-};
-MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_fwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);
-struct MapBwdLayout {
-  Pieces rows, cols;                  // sizes alone
-  int32_t parts, head_parts, list_parts;
-  size_t neg_lse2, neg_delta, row_counts, row_order, row_split, col_counts, col_order, col_split, part_q, part_k, part_v, total;
-};
-MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block);
 hipError_t launch_map_bwd(const MapArgs& a, int32_t head_dim, hipStream_t stream);
 
 }  // namespace psa

@@ -311,33 +311,6 @@ __device__ __forceinline__ int length_class(int32_t c, float mean) {
          x >= 1.25f * mean ? 4 : x >= 1.1f * mean ? 5 : x >= 0.9f * mean ? 6 : 7;
 }
 
-// The lists' lengths differ: a row of text lists every key block, a key block that every row keeps (text, the first block
-// of a sequence) lists the rows of every query head, and such a list can outlast all the others together.  So long
-// ones go in pieces, each to a workgroup of its own that leaves its sums in the workspace, where another kernel adds them.
-// With `room` workgroups sharing the work (`share` blocks each):
-//   * more items than room: lists longer than 1.25 share, in pieces of half a share, 8 blocks at least (shorter ones,
-//     started first, end with the others).  At most 0.8 room lists and 2.8 room pieces, whatever the map.
-//   * fewer: a list of average length goes in room / items pieces and a longer one in pieces as long, 4 blocks at
-//     least.  At most 4/3 room pieces.
-// Whole gradients without and with pieces, in us.  Every row keeps the first block and others by chance: 12 heads x
-// 32760 (D 128, blocks of 128, 8 kept) 1247 and 1031; 16 heads over 4 3815 and 1298; 12 x 16384 (D 64, blocks of 64, 12
-// kept) 342 and 249; 32 over 8 x 16384 (D 128, blocks of 64, 16 kept) 2060 and 1280.  Rows of text (226 tokens): 8
-// heads x 4096 (D 128, blocks of 64, 8 kept) 181 and 124.  Maps without any of these pay 0 to 2 %.
-constexpr int kPieceBlocks = 8, kFewBlocks = 4;
-struct Cut {
-  float mean, piece, longest, up;
-  __device__ __forceinline__ Cut(unsigned long long work, int32_t items, int32_t room, const Pieces& to) {
-    const float share = (float)work / (float)room;
-    mean = (float)work / (float)items;
-    const bool few = items <= room;
-    piece = few ? fmaxf((float)kFewBlocks, mean / (float)(room / items)) : fmaxf((float)kPieceBlocks, 0.5f * share);
-    longest = to.pieces == 0 ? __builtin_inff() : few ? 1.5f * piece : fmaxf(1.5f * kPieceBlocks, 1.25f * share);
-    up = few ? 0.5f : 1.0f;
-  }
-  __device__ __forceinline__ bool cuts(int32_t c) const { return (float)c > longest; }
-  __device__ __forceinline__ int32_t pieces(int32_t c) const { return (int32_t)((float)c / piece + up); }   // of such a list
-};
-
 //   order[workgroup] = (item, piece << 16 | pieces): the pieces first (a piece's tile of the workspace is its workgroup's
 //                      number), then the whole items by their lengths, then -1
 //   split[i]         = (item, workgroup of its first piece, pieces), split[-1].x their number
@@ -1087,14 +1060,6 @@ __global__ __launch_bounds__(256) void psa_mapped_sum_kernel(AllSums all) {
       *(bf16x4*)(dst + 4 * (at + 256 * u)) = __builtin_convertvector(s[u] * p.scale, bf16x4);
 }
 
-// Workgroups that share a call's work: one of 128 rows to a CU, two of 64.
-int32_t room_of(int32_t block) { return 256 * (128 / block); }
-// Forward items that run at once, twice as many at head dim 64.  No more than these are not ordered: ordered and not, 8
-// heads x 5000 take 36 and 24 us at block 64, 44 and 36 at block 128; 8 x 8000 at block 64 67 and 52.
-int32_t at_once(int32_t head_dim, int32_t block) { return room_of(block) * (128 / head_dim); }
-
-size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-
 int32_t list_bytes(int32_t nb) { return (2 * nb + 15) & ~15; }
 
 template <typename F>
@@ -1106,100 +1071,6 @@ hipError_t by_shape(int32_t head_dim, int32_t block, F f) {
 }
 
 }  // namespace
-
-// Parts of every query block's list: as many as give every CU its workgroups where there are fewer query blocks
-// (two of 64 rows to a CU, one of 128), each part at least six blocks of a full row: the parts' sums cost a kernel more, 4 us,
-// and a block 0.5 to 1.3 us.
-int32_t map_parts(int32_t n_bh, int32_t nbq, int32_t nbk, int32_t block) {
-  const int64_t items = (int64_t)n_bh * nbq, room = room_of(block);
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(room / items, nbk / 6));
-}
-
-// The order of a kernel's `items`, whose lists hold at most `longest` blocks and would else go in `parts` each.  Items that
-// all run at once (`at_once` of them) are ordered too if a part may hold more than a kernel's `long_part` tokens: the
-// order costs 10 to 20 us of a balanced call, a block of 128 takes 2.4 us in the gradients' kernels and 1 us in the
-// forward's, one of 64 half as much.  (Gradients, D 128, blocks of 64, equal parts and the order, in us: 4 heads over 2 x
-// 7791 with 226 of text, 31 kept, 337 and 228; without text 4 over 2 x 5760, 43 kept, 171 and 187; 3 heads x 2430 in a
-// batch of 4, whose lists stay below, 130 and 160.  Forward: 4 x 8192 with text, 16 kept, 119 and 66; 2 x 16384
-// without, 40 kept, 63 and 67.)
-Pieces pieces_for(int64_t items, int32_t at_once, int64_t longest, int32_t parts, int32_t long_part, int32_t block) {
-  Pieces p = {};
-  const int64_t room = room_of(block);
-  if (items <= at_once && longest / parts * block <= long_part) return p;
-  p.pieces = (int32_t)std::min(3 * room, items * ((longest + kFewBlocks - 1) / kFewBlocks));
-  p.splits = (int32_t)std::min(room, items);
-  p.grid = (int32_t)(items + p.pieces);
-  return p;
-}
-
-constexpr int32_t kLongForward = 8000, kLongBackward = 3000;
-// No forward list shorter than this goes in pieces: they cost a launch more, 5 us (20 heads x 2400 in a batch of 2, 226 of
-// text, blocks of 64: 86 and 90 us; 8 x 4096: 65 and 63; 4 x 8192: 119 and 66; 3 x 16384: 235 and 105).
-constexpr int32_t kShortForward = 6000;
-
-MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
-  MapLayout l = {};
-  l.parts = map_parts(n_bh, nbq, nbk, block);
-  // (single query blocks that all run at once: a few tokens behind a cache, lists as long as each other)
-  const int64_t items = (int64_t)n_bh * nbq;
-  const int32_t slots = at_once(head_dim, block);
-  if (nbq > 1 || items > slots) l.rows = pieces_for(items, slots, nbk, l.parts, kLongForward, block);
-  auto take = [&](size_t& at, size_t bytes) {
-    at = l.total;
-    l.total += up256(bytes);
-  };
-  if (l.rows.grid) {
-    l.parts = 1;
-    if ((int64_t)nbk * block < kShortForward) l.rows.pieces = l.rows.splits = 0, l.rows.grid = (int32_t)items;
-    take(l.row_counts, (size_t)n_bh * nbq * sizeof(int32_t));
-    take(l.row_order, l.rows.grid * sizeof(int2));
-    take(l.row_split, (1 + (size_t)l.rows.splits) * sizeof(int4));
-    if (block == 64 && items > slots) {
-      take(l.pair_counts, (size_t)n_bh * pairs_per_head(nbq) * sizeof(int32_t));
-      take(l.pair_order, (size_t)n_bh * pairs_per_head(nbq) * sizeof(int32_t));
-      take(l.paired, sizeof(int32_t));
-    }
-  }
-  const size_t tiles = l.rows.grid ? l.rows.pieces : l.parts > 1 ? (size_t)n_bh * nbq * l.parts : 0;
-  take(l.part_o, tiles * block * head_dim * sizeof(float));
-  take(l.part_ml, tiles * block * sizeof(float2));
-  return l;
-}
-
-MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
-  MapBwdLayout l = {};
-  // dq's lists go in parts as the forward's do, dk's and dv's by the query heads of a key head first; or in pieces.
-  const int32_t group = n_bh / n_kv, room = std::max(1, (int32_t)(room_of(block) / ((int64_t)n_kv * nbk)));
-  l.parts = map_parts(n_bh, nbq, nbk, block);
-  l.head_parts = std::min(group, room);
-  l.list_parts = std::max(1, std::min(room / l.head_parts, nbq / 6));
-  const int32_t kv_parts = l.head_parts * l.list_parts;
-  l.rows = pieces_for((int64_t)n_bh * nbq, room_of(block), nbk, l.parts, kLongBackward, block);
-  l.cols = pieces_for((int64_t)n_kv * nbk, room_of(block), (int64_t)group * nbq, kv_parts, kLongBackward, block);
-  const size_t tile = (size_t)block * head_dim * sizeof(float);
-  auto take = [&](size_t& at, size_t bytes) {
-    at = l.total;
-    l.total += up256(bytes);
-  };
-  take(l.neg_lse2, (size_t)n_bh * nbq * block * sizeof(float));
-  take(l.neg_delta, (size_t)n_bh * nbq * block * sizeof(float));
-  if (l.rows.grid) {
-    take(l.row_counts, (size_t)n_bh * nbq * sizeof(int32_t));
-    take(l.row_order, l.rows.grid * sizeof(int2));
-    take(l.row_split, (1 + (size_t)l.rows.splits) * sizeof(int4));
-  }
-  if (l.cols.grid) {
-    take(l.col_counts, (size_t)n_kv * nbk * sizeof(int32_t));
-    take(l.col_order, l.cols.grid * sizeof(int2));
-    take(l.col_split, (1 + (size_t)l.cols.splits) * sizeof(int4));
-  }
-  const size_t tiles_q = l.rows.grid ? l.rows.pieces : l.parts > 1 ? (size_t)n_bh * nbq * l.parts : 0;
-  const size_t tiles_kv = l.cols.grid ? l.cols.pieces : kv_parts > 1 ? (size_t)n_kv * nbk * kv_parts : 0;
-  take(l.part_q, tile * tiles_q);
-  take(l.part_k, tile * tiles_kv);
-  take(l.part_v, tile * tiles_kv);
-  return l;
-}
 
 // What comes before the main kernels: a backward call's row values, the list lengths and the orders of the rows and columns
 // that have one.
