@@ -349,7 +349,8 @@ typedef struct {
  *   norm          0: the rotation alone (the weights must be NULL)
  *   q_weight, k_weight  device fp32 [head_dim] each, or NULL for ones
  *   eps           >= 0, finite
- * head_dim 64 or 128; batch * tensors <= 65535. */
+ * head_dim 64 or 128; batch * tensors <= 65535; N <= 2^28 - 16 at head_dim 128, 2^29 - 32 at 64 (a launch numbers its
+ * threads in 32 bits: else PSA_ERR_UNSUPPORTED). */
 psa_status_t psa_qk_norm_rope_fwd(const psa_rows_t* q, const psa_rows_t* k, void* q_out, void* k_out,
                                   int32_t type, int32_t batch, int32_t head_dim, const psa_rope_t* rope,
                                   int32_t norm, const float* q_weight, const float* k_weight, float eps,
@@ -382,6 +383,12 @@ psa_status_t psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const 
  * long cache, down to one) and a key head may serve several
  * consecutive query heads.
  * Blocks are runs of `block` tokens from the first on, the last of each side partial.
+ * A launch numbers its threads in 32 bits, which bounds the blocks of all heads of a call, R = batch * n_heads *
+ * ceil(n_q / block) and C = batch * kv->n_heads * ceil(n_k / block): beyond these, PSA_ERR_UNSUPPORTED (size queries: 0).
+ *   selection   R + C < 2^24, batch * n_heads * ceil(n_q / (16 block)) < 2^23 - 8
+ *   attention   R < 2^30 / block - 2^11
+ *   gradients   the same for R and C, and R * (block * head_dim / 8 + 64) + 256 * batch * kv->n_heads *
+ *               ceil(n_k / (64 block)) < 2^32 - 2^10
  * --------------------------------------------------------------------------------------------- */
 
 /* Keys and values, bf16 [batch][n_heads][n_k][head_dim]: rows contiguous, batch elements and heads by strides in
@@ -435,8 +442,8 @@ psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, i
                                    float softmax_scale, float* lse, void* workspace,
                                    size_t workspace_bytes, hipStream_t stream);
 
-/* Bytes of device workspace of psa_attention_map_bwd (0 if invalid): at most about 150 MB, 8 bytes for every (head, query)
- * and 12 for every (head, block). */
+/* Bytes of device workspace of psa_attention_map_bwd (0 if invalid): at most about 150 MB, 8 bytes for every (head, query),
+ * the queries filled up to whole blocks, and 12 for every (head, block). */
 size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_heads,
                                             int32_t head_dim, int32_t n_q, int32_t n_k, int32_t block);
 

@@ -366,6 +366,11 @@ psa_status_t check_mapped(int32_t batch, int32_t n_heads, int32_t n_kv_heads, in
   return PSA_OK;
 }
 
+// A call whose sizes are right but whose launches would not hold them.
+psa_status_t check_launch(bool fits) {
+  return fits ? PSA_OK : fail(PSA_ERR_UNSUPPORTED, "more blocks than a launch holds");
+}
+
 psa_status_t check_kv(const psa_kv_t* kv, bool values) {
   if (!kv || !kv->k || (values && !kv->v)) return fail(PSA_ERR_INVALID, "keys and values must be non-NULL");
   if (!aligned(kv->k, 16) || (values && !aligned(kv->v, 16)))
@@ -688,6 +693,7 @@ psa_status_t psa_qk_norm_rope_fwd(const psa_rows_t* q, const psa_rows_t* k, void
   psa::RopeArgs a;
   psa_status_t s = check_rope(type, batch, k ? 2 : 1, head_dim, rope, norm, q_weight, k_weight, eps, &a);
   if (s != PSA_OK) return s;
+  if (!psa::rope_fits(a.n, head_dim)) return fail(PSA_ERR_UNSUPPORTED, "%d tokens are too many", a.n);
   if (!q) return fail(PSA_ERR_INVALID, "q is NULL");
   const psa_rows_t* rows[2] = {q, k};
   void* out[2] = {q_out, k_out};
@@ -766,7 +772,9 @@ size_t psa_select_workspace_size(int32_t batch, int32_t n_heads, int32_t n_kv_he
                                  int32_t n_q, int32_t n_k, int32_t block) {
   const SavedError keep;
   int32_t nbq, nbk;
-  if (check_mapped(batch, n_heads, n_kv_heads, head_dim, n_q, n_k, block, &nbq, &nbk) != PSA_OK) return 0;
+  if (check_mapped(batch, n_heads, n_kv_heads, head_dim, n_q, n_k, block, &nbq, &nbk) != PSA_OK ||
+      !psa::select_fits(batch * n_heads, batch * n_kv_heads, nbq, nbk))
+    return 0;
   return psa::select_layout(batch * n_heads, batch * n_kv_heads, head_dim, nbq, nbk).total;
 }
 
@@ -778,6 +786,8 @@ psa_status_t psa_select_blocks(const void* q, const psa_kv_t* kv, int32_t batch,
   if (s != PSA_OK) return s;
   psa::SelectArgs a = {};
   s = check_mapped(batch, n_heads, kv->n_heads, head_dim, n_q, n_k, block, &a.nbq, &a.nbk);
+  if (s != PSA_OK) return s;
+  s = check_launch(psa::select_fits(batch * n_heads, batch * kv->n_heads, a.nbq, a.nbk));
   if (s != PSA_OK) return s;
   if (!q || !aligned(q, 16)) return fail(PSA_ERR_INVALID, "q must be non-NULL and 16-byte aligned (%p)", q);
   if (!blockmap) return fail(PSA_ERR_INVALID, "blockmap is NULL");
@@ -817,7 +827,8 @@ size_t psa_attention_map_workspace_size(int32_t batch, int32_t n_heads, int32_t 
   const SavedError keep;
   int32_t nbq, nbk;
   if (check_mapped(batch, n_heads, 1, head_dim, n_q, n_k, block, &nbq, &nbk) != PSA_OK) return 0;
-  return psa::map_layout(batch * n_heads, head_dim, nbq, nbk, block).total;
+  const psa::MapLayout l = psa::map_layout(batch * n_heads, head_dim, nbq, nbk, block);
+  return psa::map_fits(l, batch * n_heads, nbq, block) ? l.total : 0;
 }
 
 psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, int32_t batch,
@@ -830,6 +841,8 @@ psa_status_t psa_attention_map_fwd(const void* q, const psa_kv_t* kv, void* o, i
                                   softmax_scale, &a);
   if (s != PSA_OK) return s;
   const psa::MapLayout l = psa::map_layout(a.n_bh, head_dim, a.nbq, a.nbk, block);
+  s = check_launch(psa::map_fits(l, a.n_bh, a.nbq, block));
+  if (s != PSA_OK) return s;
   s = check_map_workspace(workspace, workspace_bytes, l.total);
   if (s != PSA_OK) return s;
   a.parts = l.parts;
@@ -856,7 +869,8 @@ size_t psa_attention_map_bwd_workspace_size(int32_t batch, int32_t n_heads, int3
   const SavedError keep;
   int32_t nbq, nbk;
   if (check_mapped(batch, n_heads, n_kv_heads, head_dim, n_q, n_k, block, &nbq, &nbk) != PSA_OK) return 0;
-  return psa::map_bwd_layout(batch * n_heads, batch * n_kv_heads, head_dim, nbq, nbk, block).total;
+  const psa::MapBwdLayout l = psa::map_bwd_layout(batch * n_heads, batch * n_kv_heads, head_dim, nbq, nbk, block);
+  return psa::map_bwd_fits(l, batch * n_heads, batch * n_kv_heads, head_dim, nbq, nbk, block) ? l.total : 0;
 }
 
 psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_kv_t* kv, const void* o,
@@ -874,6 +888,8 @@ psa_status_t psa_attention_map_bwd(const void* grad_o, const void* q, const psa_
     if (!p || !aligned(p, 16))
       return fail(PSA_ERR_INVALID, "grad_o, dq, dk and dv must be non-NULL and 16-byte aligned (%p)", p);
   const psa::MapBwdLayout l = psa::map_bwd_layout(a.n_bh, batch * kv->n_heads, head_dim, a.nbq, a.nbk, block);
+  s = check_launch(psa::map_bwd_fits(l, a.n_bh, batch * kv->n_heads, head_dim, a.nbq, a.nbk, block));
+  if (s != PSA_OK) return s;
   s = check_map_workspace(workspace, workspace_bytes, l.total);
   if (s != PSA_OK) return s;
   a.grad_o = (const __bf16*)grad_o;

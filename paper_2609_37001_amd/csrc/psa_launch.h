@@ -15,6 +15,9 @@ namespace psa {
 // Number of work queues of the sparse scheduler: one per XCD of an MI355X (8 XCDs of 32 CUs).
 constexpr int kNumQueues = 8;
 
+// Whether a launch can hold so many workgroups: the threads of a grid's axis are numbered in 32 bits.
+inline bool launch_fits(int64_t groups, int32_t threads) { return groups * threads <= (int64_t)UINT32_MAX; }
+
 // Heads whose stripe parameters travel in one kernel-argument block.
 constexpr int kHeadsPerChunk = 64;
 
@@ -251,6 +254,9 @@ struct RopeArgs {
   int32_t wide, tiles, heads_per_group;   // set by the launcher
   double turns[kRopePairs];           // turns per position of every pair, theta^(-2 j / d_a) / (2 pi)
 };
+
+// Whether the forward's launch holds the tokens.
+bool rope_fits(int32_t n, int32_t head_dim);
 
 // Rows of partial sums per tensor that the backward of these sizes writes.
 int64_t rope_partial_rows(RopeArgs args, int32_t head_dim);

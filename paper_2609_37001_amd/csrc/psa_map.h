@@ -21,6 +21,8 @@ struct SelectArgs {
 struct SelectLayout {
   size_t mean_q, mean_k, scores, total;
 };
+// Whether the launches hold the blocks of both sides.
+bool select_fits(int32_t n_bh, int32_t n_kv, int32_t nbq, int32_t nbk);
 SelectLayout select_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk);
 hipError_t launch_select(const SelectArgs& args, int32_t head_dim, hipStream_t stream);
 

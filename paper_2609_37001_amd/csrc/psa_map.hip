@@ -1077,13 +1077,12 @@ hipError_t by_shape(int32_t head_dim, int32_t block, F f) {
 template <int D>
 static hipError_t launch_prepare(const MapArgs& a, bool backward, hipStream_t stream) {
   const int32_t n_kv = a.n_bh / a.group;
-  const int64_t value_groups = backward ? ((int64_t)a.n_bh * a.nbq * a.block * (D / 8) + 255) / 256 : 0;
-  const int32_t row_groups = a.row_counts ? (a.n_bh * pairs_per_head(a.nbq) + 3) / 4 : 0;
-  const int64_t col_groups = a.col_counts ? (int64_t)(a.nbk + 63) / 64 * n_kv : 0;
-  const int64_t groups = value_groups + row_groups + col_groups;
+  const int64_t values = backward ? value_groups(a.n_bh, D, a.nbq, a.block) : 0;
+  const int64_t rows = a.row_counts ? row_groups(a.n_bh, a.nbq) : 0, cols = a.col_counts ? col_groups(n_kv, a.nbk) : 0;
+  const int64_t groups = values + rows + cols;
   if (groups == 0) return hipSuccess;
-  hipLaunchKernelGGL(psa_mapped_prepare_kernel<D>, dim3((uint32_t)groups), dim3(256), 0, stream, a, (int32_t)value_groups,
-                     row_groups);
+  hipLaunchKernelGGL(psa_mapped_prepare_kernel<D>, dim3((uint32_t)groups), dim3(256), 0, stream, a, (int32_t)values,
+                     (int32_t)rows);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || (!a.row_counts && !a.col_counts)) return e;
   const Order other = backward ? Order::kCols : Order::kPairs;

@@ -118,6 +118,12 @@ inline MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t
   return l;
 }
 
+// Whether the launches of a forward hold its workgroups (those for pairs and for the list lengths are fewer).
+inline bool map_fits(const MapLayout& l, int32_t n_bh, int32_t nbq, int32_t block) {
+  const int64_t items = (int64_t)n_bh * nbq;
+  return launch_fits(l.rows.grid ? items + l.rows.pieces : items * l.parts, 4 * block);
+}
+
 struct MapBwdLayout {
   Pieces rows, cols;                  // sizes alone
   int32_t parts, head_parts, list_parts;
@@ -156,6 +162,21 @@ inline MapBwdLayout map_bwd_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim,
   take(l.part_k, tile * tiles_kv);
   take(l.part_v, tile * tiles_kv);
   return l;
+}
+
+// Workgroups of a backward call that form its row values, and that count the lists of rows and of columns.
+inline int64_t value_groups(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t block) {
+  return ((int64_t)n_bh * nbq * block * (head_dim / 8) + 255) / 256;
+}
+inline int64_t row_groups(int32_t n_bh, int32_t nbq) { return ((int64_t)n_bh * pairs_per_head(nbq) + 3) / 4; }
+inline int64_t col_groups(int32_t n_kv, int32_t nbk) { return (int64_t)(nbk + 63) / 64 * n_kv; }
+
+inline bool map_bwd_fits(const MapBwdLayout& l, int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
+  const int64_t rows = (int64_t)n_bh * nbq, cols = (int64_t)n_kv * nbk;
+  const int64_t prepare = value_groups(n_bh, head_dim, nbq, block) + (l.rows.grid ? row_groups(n_bh, nbq) : 0) +
+                          (l.cols.grid ? col_groups(n_kv, nbk) : 0);
+  return launch_fits(l.rows.grid ? rows + l.rows.pieces : rows * l.parts, 4 * block) &&
+         launch_fits(l.cols.grid ? cols + l.cols.pieces : cols * l.head_parts * l.list_parts, 4 * block) && launch_fits(prepare, 256);
 }
 
 }  // namespace psa

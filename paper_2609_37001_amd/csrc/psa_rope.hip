@@ -304,6 +304,11 @@ static void rope_split(RopeArgs& a, int32_t d, int32_t groups, int32_t* head_gro
 // 13.3 and 23.5 us, the gradients of 12 heads x 32760 124, 126 and 139.
 constexpr int32_t kRopeGroups = 2048;
 
+bool rope_fits(int32_t n, int32_t d) {
+  const int32_t rows = kRopeThreads / (d / 8);
+  return launch_fits(((int64_t)n + rows - 1) / rows, kRopeThreads);
+}
+
 int64_t rope_partial_rows(RopeArgs a, int32_t d) {
   int32_t hg;
   rope_split(a, d, kRopeGroups, &hg);

@@ -223,6 +223,14 @@ static int select_regs(int32_t first_k) {
 // Workgroups that have a slab each: two per CU.
 constexpr int32_t kSelectGroups = 512;
 
+static int64_t select_items(int32_t n_bh, int32_t nbq) {
+  return ((int64_t)n_bh * ((nbq + kSelectRows - 1) / kSelectRows) + kNumQueues - 1) / kNumQueues * kNumQueues;
+}
+
+bool select_fits(int32_t n_bh, int32_t n_kv, int32_t nbq, int32_t nbk) {
+  return launch_fits((int64_t)n_bh * nbq + (int64_t)n_kv * nbk, 256) && launch_fits(select_items(n_bh, nbq), 64 * kSelectWaves);
+}
+
 SelectLayout select_layout(int32_t n_bh, int32_t n_kv, int32_t head_dim, int32_t nbq, int32_t nbk) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   SelectLayout l;
@@ -239,7 +247,7 @@ hipError_t launch_select(const SelectArgs& args, int32_t head_dim, hipStream_t s
   SelectArgs a = args;
   a.q_blocks_all = a.n_bh * a.nbq;
   a.slab = std::max(a.first_k, 1);
-  const int32_t items = (a.n_bh * ((a.nbq + kSelectRows - 1) / kSelectRows) + kNumQueues - 1) / kNumQueues * kNumQueues;
+  const int32_t items = (int32_t)select_items(a.n_bh, a.nbq);
   const int32_t slabs = std::min(kSelectGroups, items);
   const int32_t bytes = kSelectRows * a.slab * (int32_t)sizeof(uint64_t);
   const dim3 means(a.q_blocks_all + (a.n_bh / a.group) * a.nbk);

@@ -139,3 +139,41 @@ def test_norm_rope_workspace_of_queries_alone_up_to_the_largest_batch(batch):
                                       1e-6, vp(ws), nbytes, None) == WORKSPACE
     assert L.psa_qk_norm_rope_workspace_size(65536, 1, 0, d, _lib.grid_of(1, 2, 3, 1), 1) == 0
     assert L.psa_qk_norm_rope_workspace_size(32768, 1, 1, d, _lib.grid_of(1, 2, 3, 1), 1) == 0
+
+
+def status(kind, batch, d, block, ws=256, wsb=16):
+    """One query and one key of every (batch element, head), four heads over two, in too small a workspace."""
+    s = dict(batch=batch, d=d, block=block, n_q=1, n_k=1, ws=ws, wsb=wsb)
+    return dict(select=select, forward=mapped, backward=mapped_bwd)[kind](**s)
+
+
+def size(kind, batch, d, block):
+    L = _lib.lib()
+    if kind == "forward":
+        return L.psa_attention_map_workspace_size(batch, 4, d, 1, 1, block)
+    return (L.psa_select_workspace_size if kind == "select" else L.psa_attention_map_bwd_workspace_size)(
+        batch, 4, 2, d, 1, 1, block)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("block", [64, 128])
+@pytest.mark.parametrize("kind", ["select", "forward", "backward"])
+def test_calls_that_no_launch_holds(kind, d, block):
+    """The threads of a launch are numbered in 32 bits: sizes beyond are refused before anything is started, and the
+    largest below pass on to the check of the workspace."""
+    rows = {"select": (2 ** 32 - 1) // 512,                          # 8 waves for 16 query blocks of one head
+            "forward": (2 ** 32 - 1) // (4 * block) - 2 ** 10,       # 4 block threads a query block, and those of pieces
+            # (a thread for eight channels of a padded row, a wave a row and four a key head for the list lengths)
+            "backward": min((2 ** 32 - 1) // (4 * block) - 2 ** 11, 2 ** 32 // (block * d // 8 + 64 + 256 // 2))}[kind]
+    assert status(kind, rows // 4 - 8, d, block) == WORKSPACE and size(kind, rows // 4 - 8, d, block) > 0
+    for more in (rows // 4 + 2 ** 10, rows // 2, rows):
+        assert status(kind, more, d, block) == UNSUPPORTED and size(kind, more, d, block) == 0
+
+
+@pytest.mark.parametrize("d,most", [(64, 2 ** 29 - 32), (128, 2 ** 28 - 16)])
+def test_norm_rope_tokens_that_no_launch_holds(d, most):
+    axes = (24, 20, 20) if d == 64 else (44, 42, 42)
+    x = rows(x=0, b=0, h=0, n=d, heads=1)
+    assert fwd(q=x, k=None, d=d, r=rope((1, 1, most, 0), axes=axes)) == INVALID       # (q.x is NULL)
+    assert fwd(q=x, k=None, d=d, r=rope((1, 1, most + 1, 0), axes=axes)) == UNSUPPORTED
+    assert fwd(q=x, k=None, d=d, r=rope((1, 1, most - 5, 6), axes=axes)) == UNSUPPORTED
