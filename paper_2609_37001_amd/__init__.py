@@ -446,6 +446,14 @@ def l2_distance(o, ref, sq_err=None, sq_ref=None, workspace=None, stream=None):
 # Norms and rotary positions of queries and keys (include/psa.h, fourth part).
 # ---------------------------------------------------------------------------------------------
 
+def _int32(x, name):
+    """A whole number for a 32-bit argument of the library (ctypes would hand on the low bits of a larger one)."""
+    x = int(x)
+    if not -0x80000000 <= x <= 0x7fffffff:
+        raise ValueError("%s %d is not a number of 32 bits" % (name, x))
+    return x
+
+
 def _on_device(device, stream):
     """Contexts of a call: the tensors' device and the stream given.  Nothing to enter where both are the current
     ones (two contexts cost as much host time as the launch of a small call)."""
@@ -484,7 +492,7 @@ def _rows(x, name, dtype, tokens, like=None):
 def _rope(grid, axes, theta, origin, pairing):
     if pairing not in ("adjacent", "halves"):
         raise ValueError('pairing is "adjacent" or "halves"')
-    a, o = tuple(map(int, axes)), tuple(map(int, origin))
+    a, o = tuple(_int32(x, "axis") for x in axes), tuple(_int32(x, "origin") for x in origin)
     if len(a) != 3 or len(o) != 3:
         raise ValueError("axes and origin have three entries (time, height, width)")
     return _lib.Rope(_grid(grid), *o, *a, _lib.PAIRS_HALVES if pairing == "halves" else _lib.PAIRS_ADJACENT, theta)
@@ -636,7 +644,7 @@ def _kv(q, k, v=None):
 
 
 def _blocks(n, block):
-    return -(-n // int(block)) if int(block) > 0 else 0
+    return -(-n // block) if block > 0 else 0
 
 
 def _map_of(blockmap, q, n_k, block):
@@ -674,6 +682,8 @@ def select_blocks(q, k, block, keep, q_text=0, k_text=0, blockmap=None, workspac
 
     Returns (map uint8 [batch, heads, nbq, nbk], kept_per_row int32 [batch, heads, nbq])."""
     torch = _torch()
+    block, keep = _int32(block, "block"), _int32(keep, "keep")
+    q_text, k_text = _int32(q_text, "q_text"), _int32(k_text, "k_text")
     _check_q(q)
     kv = _kv(q, k)
     b, h, n_q, d = q.shape
@@ -685,8 +695,8 @@ def select_blocks(q, k, block, keep, q_text=0, k_text=0, blockmap=None, workspac
             raise ValueError("blockmap must be a contiguous uint8 tensor %s on the queries' device" % (shape,))
         kept = torch.empty(shape[:3], dtype=torch.int32, device=q.device)
         L = _lib.lib()
-        ws, nbytes, _keep = _workspace(workspace, int(L.psa_select_workspace_size(b, h, k.shape[1], d, n_q, n_k, int(block))), q.device)
-        _lib.check(L.psa_select_blocks(_ptr(q), kv, b, h, d, n_q, n_k, int(block), int(keep), int(q_text), int(k_text),
+        ws, nbytes, _keep = _workspace(workspace, int(L.psa_select_workspace_size(b, h, k.shape[1], d, n_q, n_k, block)), q.device)
+        _lib.check(L.psa_select_blocks(_ptr(q), kv, b, h, d, n_q, n_k, block, keep, q_text, k_text,
                                        _ptr(m), _ptr(kept), ws, nbytes, _stream(None, q.device.index)))
     return m, kept
 
@@ -700,6 +710,7 @@ def attention_map_fwd(q, k, v, blockmap, block, scale=None, out=None, return_lse
 
     Returns o like q (and lse float32 [batch, heads, N_q] if asked)."""
     torch = _torch()
+    block = _int32(block, "block")
     _check_q(q)
     kv = _kv(q, k, v)
     b, h, n_q, d = q.shape
@@ -711,8 +722,8 @@ def attention_map_fwd(q, k, v, blockmap, block, scale=None, out=None, return_lse
         _check_q(o, "out", q)
         lse = torch.empty((b, h, n_q), dtype=torch.float32, device=q.device) if return_lse else None
         L = _lib.lib()
-        ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_workspace_size(b, h, d, n_q, n_k, int(block))), q.device)
-        _lib.check(L.psa_attention_map_fwd(_ptr(q), kv, _ptr(o), b, h, d, n_q, n_k, int(block), bm, bm_stride, scale,
+        ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_workspace_size(b, h, d, n_q, n_k, block)), q.device)
+        _lib.check(L.psa_attention_map_fwd(_ptr(q), kv, _ptr(o), b, h, d, n_q, n_k, block, bm, bm_stride, scale,
                                            _ptr(lse), ws, nbytes, _stream(None, q.device.index)))
     return (o, lse) if return_lse else o
 
@@ -723,6 +734,7 @@ def attention_map_bwd(do, q, k, v, o, lse, blockmap, block, scale=None, dq=None,
     lse; the other arguments are the forward's.  Returns (dq, dk, dv), contiguous; those of a shared key head are
     the sums over its query heads."""
     torch = _torch()
+    block = _int32(block, "block")
     _check_q(q)
     _check_q(do, "do", q)
     _check_q(o, "o", q)
@@ -741,8 +753,8 @@ def attention_map_bwd(do, q, k, v, o, lse, blockmap, block, scale=None, dq=None,
         _check_q(dk, "dk", k)
         _check_q(dv, "dv", k)
         L = _lib.lib()
-        ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_bwd_workspace_size(b, h, k.shape[1], d, n_q, n_k, int(block))), q.device)
-        _lib.check(L.psa_attention_map_bwd(_ptr(do), _ptr(q), kv, _ptr(o), _ptr(lse), b, h, d, n_q, n_k, int(block), bm,
+        ws, nbytes, _keep = _workspace(workspace, int(L.psa_attention_map_bwd_workspace_size(b, h, k.shape[1], d, n_q, n_k, block)), q.device)
+        _lib.check(L.psa_attention_map_bwd(_ptr(do), _ptr(q), kv, _ptr(o), _ptr(lse), b, h, d, n_q, n_k, block, bm,
                                            bm_stride, scale, _ptr(dq), _ptr(dk), _ptr(dv), ws, nbytes,
                                            _stream(None, q.device.index)))
     return dq, dk, dv

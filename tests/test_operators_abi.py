@@ -177,3 +177,23 @@ def test_norm_rope_tokens_that_no_launch_holds(d, most):
     assert fwd(q=x, k=None, d=d, r=rope((1, 1, most, 0), axes=axes)) == INVALID       # (q.x is NULL)
     assert fwd(q=x, k=None, d=d, r=rope((1, 1, most + 1, 0), axes=axes)) == UNSUPPORTED
     assert fwd(q=x, k=None, d=d, r=rope((1, 1, most - 5, 6), axes=axes)) == UNSUPPORTED
+
+
+def test_numbers_that_32_bits_do_not_hold_are_refused():
+    """The C ABI takes 32-bit numbers; the binding does not hand on what is left of larger ones."""
+    import torch
+
+    import paper_2609_37001_amd as psa
+    x, m = torch.zeros(1, 1, 64, 64).bfloat16(), torch.zeros(1, 1, 1, 1, dtype=torch.uint8)
+    lse, big = torch.zeros(1, 1, 64), 2 ** 32
+    r = psa._rope((1, 2, 3), (24, 20, 20), 1e4, (2 ** 31 - 4, -2 ** 31, 0), "adjacent")
+    assert (r.origin_t, r.origin_h, r.axis_w) == (2 ** 31 - 4, -2 ** 31, 20)
+    for call in (lambda: psa._rope((1, 2, 3), (24, 20, 20), 1e4, (0, big + 5, 0), "adjacent"),
+                 lambda: psa._rope((1, 2, 3), (24, 20, 20), 1e4, (0, -big, 0), "adjacent"),
+                 lambda: psa._rope((1, 2, 3), (big + 24, 20, 20), 1e4, (0, 0, 0), "adjacent"),
+                 lambda: psa.select_blocks(x, x, big + 64, 1), lambda: psa.select_blocks(x, x, 64, big),
+                 lambda: psa.select_blocks(x, x, 64, 1, q_text=big), lambda: psa.select_blocks(x, x, 64, 1, k_text=-big),
+                 lambda: psa.attention_map_fwd(x, x, x, m, big + 64),
+                 lambda: psa.attention_map_bwd(x, x, x, x, x, lse, m, big + 64)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
