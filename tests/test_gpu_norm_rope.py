@@ -238,3 +238,20 @@ def test_queries_alone_in_a_large_batch():
     near(dq, dx, r * (gw.max(-1, keepdims=True) + u.max(-1, keepdims=True) * (gw * u).mean(-1, keepdims=True)), 2.0 ** -8)
     terms = np.abs(g * xn * r).reshape(-1, d).sum(0)
     assert (np.abs(dw.double().cpu().numpy() - dref) <= 2.0 ** -16 * terms + 2.0 ** -24 * np.abs(dref)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("pairing", ["adjacent", "halves"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_kernel(d, pairing, norm, dtype):
+    """Every kernel of both directions (without a norm the backward holds twice the rows in flight and reads no x),
+    on a part of a tile, and on more tiles than workgroups take at once, with fewer key heads, text and a later chunk's
+    positions."""
+    check(2, 3, 1, (1, 3, 7, 2), d, dtype, "fused", norm, pairing=pairing, origin=(0, -2, 3), seed=1)
+    check(8, 2, 1, (3, 27, 51, 77), d, dtype, "bnhd", norm, pairing=pairing, origin=(21, 0, 0), seed=2)
+
+
+def test_a_later_chunk_in_32_bits():
+    """Two prompts, an odd grid, seven key heads for 28, channels paired across the halves, no norm."""
+    check(2, 28, 7, (5, 23, 37, 77), 128, "fp32", norm=False, pairing="halves", origin=(21, 0, 0), seed=3)
