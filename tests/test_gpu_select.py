@@ -136,3 +136,20 @@ def test_side_stream_and_graph_replays_match_eager():
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
+@pytest.mark.parametrize("block", [64, 128])
+@pytest.mark.parametrize("blocks_k", [321, 591, 624, 625, 1280, 1281])
+def test_long_keys_of_wide_heads(blocks_k, block):
+    """Head dim 128 in every form of the scores: 10 words a lane from LDS, 20 from the workspace, read again."""
+    n_k = blocks_k * block - 5
+    check(1, 2, 1, 17 * block + 3, n_k, 128, block, 97, heads=[1])
+    check(1, 1, 1, 40, n_k, 128, block, blocks_k - 20, k_text=200)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("blocks_k", [630, 1290])
+def test_more_rows_than_workgroups_with_a_slab(d, blocks_k):
+    """Workgroups that take several groups of 16 query blocks one after the other, their scores in the same place."""
+    check(1, 700, 1, 90, blocks_k * 64 - 30, d, 64, 41, heads=[0, 1, 349, 511, 512, 520, 699])
+    check(2, 15, 3, 300 * 64 - 7, blocks_k * 64, d, 64, 300, q_text=70, k_text=70, heads=[0, 14])
