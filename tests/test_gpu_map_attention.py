@@ -494,3 +494,37 @@ def test_replays_over_other_maps(d, block, h, hk, n):
         assert all(torch.equal(a, b) for a, b in zip(got, ref))
     check_forward(bits(q), bits(k), bits(v), m, block, d ** -0.5, bits(got[0]), got[1].cpu().numpy(), [h - 1])
     check_backward(bits(q), bits(k), bits(v), bits(do), m, block, d ** -0.5, bits(got[0]), got[1].cpu().numpy(), got[2:], [h - 1])
+
+
+def test_longest_maps_of_wide_heads():
+    """7936 blocks of 128 at head dim 128, where tiles and list take the most LDS: few queries over long keys and the reverse,
+    against the attention over the kept blocks alone."""
+    torch = gu.torch()
+    d = block = 128
+    nb = 7936
+    long = torch.randn(1, 1, nb * block, d, device="cuda:0").bfloat16()
+    short = torch.randn(1, 1, 150, d, device="cuda:0").bfloat16()
+    m, kept = psa.select_blocks(short, long, block, 21)
+    assert (kept == 21).all() and (m.sum(3) == 21).all()
+    mn = m.cpu().numpy()
+    at = np.unique(np.nonzero(mn[0, 0])[1])
+    kept_rows = torch.from_numpy((at[:, None] * block + np.arange(block)).reshape(-1)).to("cuda:0")
+    few = bits(long[:, :, kept_rows])
+    cut = mn[..., at]
+    do = torch.randn_like(short)
+    o, lse = psa.attention_map_fwd(short, long, long, m, block, return_lse=True)
+    g = psa.attention_map_bwd(do, short, long, long, o, lse, m, block)
+    rest = torch.ones(nb, dtype=torch.bool, device="cuda:0")
+    rest[torch.from_numpy(at).to("cuda:0")] = False
+    assert not any(x.view(nb, block, d)[rest].any() for x in g[1:])
+    check_forward(bits(short), few, few, cut, block, d ** -0.5, bits(o), lse.cpu().numpy(), [0])
+    check_backward(bits(short), few, few, bits(do), cut, block, d ** -0.5, bits(o), lse.cpu().numpy(),
+                   (g[0], g[1][:, :, kept_rows], g[2][:, :, kept_rows]), [0])
+    mt = m.transpose(2, 3).contiguous()
+    o, lse = psa.attention_map_fwd(long, short, short, mt, block, return_lse=True)
+    g = psa.attention_map_bwd(long, long, short, short, o, lse, mt, block)
+    assert not o.view(nb, block, d)[rest].any() and torch.isneginf(lse.view(nb, block)[rest]).all() and not g[0].view(nb, block, d)[rest].any()
+    on, ln = bits(o[:, :, kept_rows]), lse[:, :, kept_rows].cpu().numpy()
+    check_forward(few, bits(short), bits(short), cut.transpose(0, 1, 3, 2), block, d ** -0.5, on, ln, [0])
+    check_backward(few, bits(short), bits(short), few, cut.transpose(0, 1, 3, 2), block, d ** -0.5, on, ln,
+                   (g[0][:, :, kept_rows], g[1], g[2]), [0])
