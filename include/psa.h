@@ -363,8 +363,8 @@ size_t psa_qk_norm_rope_workspace_size(int32_t batch, int32_t n_heads, int32_t n
 /* Gradients of psa_qk_norm_rope_fwd.
  *   dq_out, dk_out  gradients of q_out and k_out, in their layout (bf16)
  *   q, k            the forward's rows (without a norm their x may be NULL); k NULL: queries alone
- *   dq, dk          rows that receive the gradients, in type `type`, strides of their own (none 0 where
- *                   there is more than one row to write)
+ *   dq, dk          rows that receive the gradients, in type `type`, strides of their own by which no two rows
+ *                   share memory (else PSA_ERR_INVALID; each axis steps over all that those of smaller strides reach)
  *   dq_weight, dk_weight  device fp32 [head_dim], written: with a norm required (whether the weights were
  *                   NULL or not), without one ignored
  *   workspace       device, psa_qk_norm_rope_workspace_size() bytes, 256-byte aligned (NULL without a norm)

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <utility>
 
 #include "psa_launch.h"
 #include "psa_map.h"
@@ -263,8 +264,23 @@ psa_status_t run_planned(const void* q, const void* k, const void* v, void* o, i
   return PSA_OK;
 }
 
+// Whether no two rows share memory: of the axes with more than one place, in the order of their strides, each
+// steps over all that the smaller ones reach.
+bool rows_apart(const psa_rows_t& r, int32_t batch, int64_t n, int32_t head_dim) {
+  std::pair<int64_t, int64_t> axes[3] = {{r.stride_b, batch}, {r.stride_h, r.n_heads}, {r.stride_n, n}};
+  std::sort(axes, axes + 3);
+  __int128 reach = head_dim;
+  for (const auto& a : axes) {
+    if (a.second == 1) continue;
+    if (a.first < reach) return false;
+    reach += (__int128)a.first * (a.second - 1);
+  }
+  return true;
+}
+
 // One tensor of a norm-and-rotation call.  write: the rows are an output.
-psa_status_t check_rows(const psa_rows_t& r, const char* what, int32_t batch, int64_t n, int32_t type, bool write) {
+psa_status_t check_rows(const psa_rows_t& r, const char* what, int32_t batch, int64_t n, int32_t head_dim, int32_t type,
+                        bool write) {
   const int64_t unit = type == PSA_TYPE_BF16 ? 8 : 4;       // elements of 16 bytes
   if (!r.x) return fail(PSA_ERR_INVALID, "%s is NULL", what);
   if (!aligned(r.x, 16)) return fail(PSA_ERR_INVALID, "%s must be 16-byte aligned (%p)", what, r.x);
@@ -272,7 +288,7 @@ psa_status_t check_rows(const psa_rows_t& r, const char* what, int32_t batch, in
   if (r.stride_b % unit || r.stride_h % unit || r.stride_n % unit || r.stride_b < 0 || r.stride_h < 0 || r.stride_n < 0)
     return fail(PSA_ERR_INVALID, "%s: strides must be multiples of 16 bytes, not negative (%lld, %lld, %lld)", what,
                 (long long)r.stride_b, (long long)r.stride_h, (long long)r.stride_n);
-  if (write && ((batch > 1 && !r.stride_b) || (r.n_heads > 1 && !r.stride_h) || (n > 1 && !r.stride_n)))
+  if (write && !rows_apart(r, batch, n, head_dim))
     return fail(PSA_ERR_INVALID, "%s: an output's rows must not share memory", what);
   return PSA_OK;
 }
@@ -698,7 +714,7 @@ psa_status_t psa_qk_norm_rope_fwd(const psa_rows_t* q, const psa_rows_t* k, void
   const psa_rows_t* rows[2] = {q, k};
   void* out[2] = {q_out, k_out};
   for (int i = 0; i < a.n_tensors; i++) {
-    s = check_rows(*rows[i], i ? "k" : "q", batch, a.n, type, false);
+    s = check_rows(*rows[i], i ? "k" : "q", batch, a.n, head_dim, type, false);
     if (s != PSA_OK) return s;
     if (!out[i] || !aligned(out[i], 16))
       return fail(PSA_ERR_INVALID, "outputs must be non-NULL and 16-byte aligned (%p)", out[i]);
@@ -740,12 +756,12 @@ psa_status_t psa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const 
   float* dw[2] = {dq_weight, dk_weight};
   for (int i = 0; i < a.n_tensors; i++) {
     if (norm) {
-      s = check_rows(*rows[i], i ? "k" : "q", batch, a.n, type, false);
+      s = check_rows(*rows[i], i ? "k" : "q", batch, a.n, head_dim, type, false);
       if (s != PSA_OK) return s;
       if (!dw[i] || !aligned(dw[i], 4))
         return fail(PSA_ERR_INVALID, "the weights' gradients must be non-NULL and 4-byte aligned (%p)", (void*)dw[i]);
     }
-    s = check_rows(*grads[i], i ? "dk" : "dq", batch, a.n, type, true);
+    s = check_rows(*grads[i], i ? "dk" : "dq", batch, a.n, head_dim, type, true);
     if (s != PSA_OK) return s;
     if (grads[i]->n_heads != rows[i]->n_heads)
       return fail(PSA_ERR_INVALID, "gradients of %d heads for %d", grads[i]->n_heads, rows[i]->n_heads);

@@ -197,3 +197,20 @@ def test_numbers_that_32_bits_do_not_hold_are_refused():
                  lambda: psa.attention_map_bwd(x, x, x, x, x, lse, m, big + 64)):
         with pytest.raises(ValueError, match="32 bits"):
             call()
+
+
+@pytest.mark.parametrize("bad", [rows(n=32), rows(h=64, n=64), rows(h=64, n=128, heads=3), rows(b=512, h=768, n=64),
+                                 rows(b=64 * 15, h=512, n=64), rows(b=0), rows(h=0), rows(n=0)])
+def test_outputs_whose_rows_overlap_are_refused(bad):
+    """Two batch elements, two heads and eight tokens: rows that reach into each other cannot all be written."""
+    r, g = rope((1, 1, 8, 0)), rows(heads=bad.n_heads)
+    assert _lib.lib().psa_qk_norm_rope_bwd(vp(256), None, g, None, bad, None, vp(256), None, 0, 2, 64, r, 1, None, None, 1e-6,
+                                           None, 0, None) == INVALID
+
+
+@pytest.mark.parametrize("x", [rows(b=1024, h=512, n=64), rows(b=512, h=1024, n=64), rows(b=1024, h=64, n=128), rows(b=64, h=1024, n=128), rows(b=128, h=64, n=256),
+                               rows(b=4096, h=192, n=384), rows(b=1 << 40, h=1 << 33, n=1 << 20)])
+def test_outputs_of_any_order_and_spacing_are_taken(x):
+    r = rope((1, 1, 8, 0))
+    assert _lib.lib().psa_qk_norm_rope_bwd(vp(256), None, rows(), None, x, None, vp(256), None, 0, 2, 64, r, 1, None, None, 1e-6,
+                                           None, 0, None) == WORKSPACE
