@@ -460,6 +460,8 @@ def _on_device(device, stream):
     torch = _torch()
     if stream is None and device.index == torch.cuda.current_device():
         return contextlib.nullcontext()
+    if stream is not None and stream.device != device:
+        raise ValueError("the stream is on %s, the tensors on %s" % (stream.device, device))
     stack = contextlib.ExitStack()
     stack.enter_context(torch.cuda.device(device))
     stack.enter_context(_on(stream))

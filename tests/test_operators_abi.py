@@ -214,3 +214,16 @@ def test_outputs_of_any_order_and_spacing_are_taken(x):
     r = rope((1, 1, 8, 0))
     assert _lib.lib().psa_qk_norm_rope_bwd(vp(256), None, rows(), None, x, None, vp(256), None, 0, 2, 64, r, 1, None, None, 1e-6,
                                            None, 0, None) == WORKSPACE
+
+
+def test_a_stream_of_another_device_is_refused():
+    """The launch would go to the tensors' device on a stream of another one."""
+    import torch
+
+    import paper_2609_37001_amd as psa
+
+    class Stream:
+        device = torch.device("cuda", 1)
+
+    with pytest.raises(ValueError, match="stream"):
+        psa._on_device(torch.device("cuda", 0), Stream())
