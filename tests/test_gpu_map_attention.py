@@ -528,3 +528,49 @@ def test_longest_maps_of_wide_heads():
     check_forward(few, bits(short), bits(short), cut.transpose(0, 1, 3, 2), block, d ** -0.5, on, ln, [0])
     check_backward(few, bits(short), bits(short), few, cut.transpose(0, 1, 3, 2), block, d ** -0.5, on, ln,
                    (g[0][:, :, kept_rows], g[1], g[2]), [0])
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
+@pytest.mark.parametrize("h,hk,nq,nk", [(2, 1, 3, 9), (2, 2, 40, 7), (80, 40, 17, 6), (4, 2, 21, 130)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_values_that_are_not_finite_stay_where_they_are_kept(d, block, h, hk, nq, nk, bad):
+    """A key block that the odd query blocks alone keep, one that nobody keeps, a query block that keeps nothing and one that
+    keeps the second key block alone: what is not finite there changes no other row's bits."""
+    torch = gu.torch()
+    print(d, block, h, hk, nq, nk, flush=True)
+    m = random_map(71, 1, h, nq, nk, 0.5)
+    m[..., 0], m[..., 2], m[:, :, 0], m[..., 3] = 1, 0, 0, 0
+    m[:, :, 1::2, 3] = 1
+    m[:, :, 2] = 0
+    m[:, :, 2, 4] = 1
+    n_q, n_k = nq * block - 3, nk * block - 5
+    clean = [dev(x) for x in inputs(72, 1, h, hk, n_q, n_k, d)]
+    dm = torch.from_numpy(m).to("cuda:0")
+
+    def run(t):
+        o, lse = psa.attention_map_fwd(t[0], t[1], t[2], dm, block, return_lse=True)
+        return (o, lse) + psa.attention_map_bwd(t[3], t[0], t[1], t[2], o, lse, dm, block)
+
+    ref = run(clean)
+    rows = torch.arange(n_q, device="cuda:0") // block
+    keys = torch.arange(n_k, device="cuda:0") // block
+    t = [x.clone() for x in clean]
+    for x in t[1:3]:                                    # keys and values
+        x[:, :, keys == 2] = bad
+        x[:, :, 3 * block + 7] = bad
+    for x in (t[0], t[3]):                              # queries and the gradient: rows that keep nothing
+        x[:, :, rows == 0] = bad
+    got = run(t)
+    even = (rows % 2 == 0) & (rows != 0)
+    for i in (0, 1, 2):
+        assert torch.equal(got[i][:, :, even], ref[i][:, :, even])
+    assert not got[0][:, :, rows == 0].any() and torch.isneginf(got[1][:, :, rows == 0]).all() and not got[2][:, :, rows == 0].any()
+    assert not got[3][:, :, keys == 2].any() and not got[4][:, :, keys == 2].any()
+    t = [x.clone() for x in clean]
+    t[0][:, :, 2 * block + 9] = bad                     # a query that keeps key block 4 alone
+    t[3][:, :, 2 * block + 9] = bad
+    got = run(t)
+    for i in (0, 1, 2):
+        assert torch.equal(got[i][:, :, rows != 2], ref[i][:, :, rows != 2])
+    for i in (3, 4):
+        assert torch.equal(got[i][:, :, keys != 4], ref[i][:, :, keys != 4])
