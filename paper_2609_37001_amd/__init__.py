@@ -28,6 +28,9 @@ Attention over a map of blocks that a score of the data selects (or over any oth
     bmap, kept = select_blocks(q, k, block=128, keep=64)
     o, lse = attention_map_fwd(q, k, v, bmap, block=128, return_lse=True)
     dq, dk, dv = attention_map_bwd(do, q, k, v, o, lse, bmap, block=128)
+
+No call records anything for autograd: the tensors returned have no graph, also where inputs require gradients.  The
+gradients are calls of their own (`*_bwd`).
 """
 import contextlib
 import math

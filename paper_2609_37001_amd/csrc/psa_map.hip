@@ -6,9 +6,17 @@
 //
 // Scores are exact up to their fp32 sums, in both directions: the forward scales q by a power of two alone (no
 // rounding) and multiplies every score by the rest of scale log2(e), a factor in [1, 2), before its exponential; the
-// backward multiplies by the whole.  Rounding scale log2(e) q to bf16 instead would save that multiplication (4 to 6 %
-// of the forward's time, 2 % of the backward's) and move scores by up to 2^-8 of the magnitudes they add: outputs
+// backward multiplies by the whole.  Rounding scale log2(e) q to bf16 instead would save that multiplication (3 to 6 %
+// of the forward's time, 2 % of the backward's: 5 heads x 75600, 141 blocks of 128 kept, 3335 us without and 3445 with;
+// gradients of 12 x 32760, 64 kept, 5210 and 5290) and move scores by up to 2^-8 of the magnitudes they add: outputs
 // then are 2.9e-3 off instead of 2.35e-3, and a normaliser of rows whose scores share a large part by tenths.
+//
+// Rounded to bf16, as in the library's other attention kernels: the weights P and, in the backward, dS, which the matrix
+// cores take as operands of the second products.  It is half a step, 2^-8 of a weight at most, and moves outputs by 1.6e-3; with
+// the rounding of the output, 1.65e-3, the forward is 2.3e-3 off where weights in 32 bits would leave 1.65e-3.  The
+// normaliser sums the rounded weights, so that a row's weights still add up to one.  Without it every weight
+// would be two bf16 halves and P V two products for one, three in the forward for two.  Scores, statistics
+// and all sums are in 32 bits.
 //
 // One workgroup takes one block of one side -- queries in the forward and for dq, keys for dk and dv -- holds its
 // rows in registers, and streams the blocks that the map keeps of the other side through LDS, double-buffered,
@@ -82,6 +90,7 @@ __device__ __forceinline__ int32_t item_of(int32_t blk, int32_t items) {
 // that one block of a pair or both keep, `single` those that each keeps, over all pairs.  A wave waits while its
 // neighbour's block alone is worked on, so at head dim 128 pairs pay where neighbours share enough; at head dim 64 its
 // four waves per SIMD cover such waits.  Microseconds in pairs and one by one at either / single 0.87, 0.70 and 0.50:
+// (one by one at head dim 64 on two waves per SIMD, what its attribute allows)
 //   head dim 64   12 heads x 32760, density 0.25 (256 pairs each)  1104, 1009, 895 and 1281, 1284, 1288
 //                 16 x 8000, 0.2 (63 pairs each)                   107, 94, 85     and 118, 118, 116
 //                 9 x 8000, 0.2                                    90, 81, 67      and 91, 88, 87

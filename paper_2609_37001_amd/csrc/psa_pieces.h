@@ -48,9 +48,10 @@ struct Cut {
 
 // Workgroups that share a call's work: one of 128 rows to a CU, two of 64.
 inline int32_t room_of(int32_t block) { return 256 * (128 / block); }
-// Forward items that run at once, twice as many at head dim 64.  No more than these are not ordered: ordered and not, 8
-// heads x 5000 take 36 and 24 us at block 64, 44 and 36 at block 128; 8 x 8000 at block 64 67 and 52.
-inline int32_t at_once(int32_t head_dim, int32_t block) { return room_of(block) * (128 / head_dim); }
+// Forward items up to which a call is not ordered: as many as run at once, at head dim 64 twice as many (two rounds: the
+// kernel there is held to two waves per SIMD, though its registers and LDS would allow four).  Ordered and not at head
+// dim 64, 8 heads x 5000 take 36 and 24 us at block 64, 44 and 36 at block 128; 8 x 8000 at block 64 67 and 52.
+inline int32_t unordered(int32_t head_dim, int32_t block) { return room_of(block) * (128 / head_dim); }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -62,17 +63,17 @@ inline int32_t map_parts(int32_t n_bh, int32_t nbq, int32_t nbk, int32_t block) 
   return (int32_t)std::max<int64_t>(1, std::min<int64_t>(room / items, nbk / 6));
 }
 
-// The order of a kernel's `items`, whose lists hold at most `longest` blocks and would else go in `parts` each.  Items that
-// all run at once (`at_once` of them) are ordered too if a part may hold more than a kernel's `long_part` tokens: the
+// The order of a kernel's `items`, whose lists hold at most `longest` blocks and would else go in `parts` each.  No more than
+// `unordered` items are ordered too if a part may hold more than a kernel's `long_part` tokens: the
 // order costs 10 to 20 us of a balanced call, a block of 128 takes 2.4 us in the gradients' kernels and 1 us in the
 // forward's, one of 64 half as much.  (Gradients, D 128, blocks of 64, equal parts and the order, in us: 4 heads over 2 x
 // 7791 with 226 of text, 31 kept, 337 and 228; without text 4 over 2 x 5760, 43 kept, 171 and 187; 3 heads x 2430 in a
 // batch of 4, whose lists stay below, 130 and 160.  Forward: 4 x 8192 with text, 16 kept, 119 and 66; 2 x 16384
 // without, 40 kept, 63 and 67.)
-inline Pieces pieces_for(int64_t items, int32_t at_once, int64_t longest, int32_t parts, int32_t long_part, int32_t block) {
+inline Pieces pieces_for(int64_t items, int32_t unordered, int64_t longest, int32_t parts, int32_t long_part, int32_t block) {
   Pieces p = {};
   const int64_t room = room_of(block);
-  if (items <= at_once && longest / parts * block <= long_part) return p;
+  if (items <= unordered && longest / parts * block <= long_part) return p;
   p.pieces = (int32_t)std::min(3 * room, items * ((longest + kFewBlocks - 1) / kFewBlocks));
   p.splits = (int32_t)std::min(room, items);
   p.grid = (int32_t)(items + p.pieces);
@@ -80,8 +81,9 @@ inline Pieces pieces_for(int64_t items, int32_t at_once, int64_t longest, int32_
 }
 
 constexpr int32_t kLongForward = 8000, kLongBackward = 3000;
-// No forward list shorter than this goes in pieces: they cost a launch more, 5 us (20 heads x 2400 in a batch of 2, 226 of
-// text, blocks of 64: 86 and 90 us; 8 x 4096: 65 and 63; 4 x 8192: 119 and 66; 3 x 16384: 235 and 105).
+// No forward list shorter than this goes in pieces: they cost a launch more, 5 us (without and with them, 226 of text,
+// blocks of 64: 20 heads x 2400 in a batch of 2 86 and 90 us; 8 x 4096 65 and 63; 4 x 8192 119 and 66; 3 x 16384 235
+// and 105.  Nothing between 4096 and 8192 was measured.)
 constexpr int32_t kShortForward = 6000;
 
 struct MapLayout {
@@ -92,9 +94,9 @@ struct MapLayout {
 inline MapLayout map_layout(int32_t n_bh, int32_t head_dim, int32_t nbq, int32_t nbk, int32_t block) {
   MapLayout l = {};
   l.parts = map_parts(n_bh, nbq, nbk, block);
-  // (single query blocks that all run at once: a few tokens behind a cache, lists as long as each other)
+  // (single query blocks, no more than `slots`: a few tokens behind a cache, lists as long as each other)
   const int64_t items = (int64_t)n_bh * nbq;
-  const int32_t slots = at_once(head_dim, block);
+  const int32_t slots = unordered(head_dim, block);
   if (nbq > 1 || items > slots) l.rows = pieces_for(items, slots, nbk, l.parts, kLongForward, block);
   auto take = [&](size_t& at, size_t bytes) {
     at = l.total;
