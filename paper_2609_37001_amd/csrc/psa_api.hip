@@ -376,8 +376,9 @@ psa_status_t check_mapped(int32_t batch, int32_t n_heads, int32_t n_kv_heads, in
   *nbk = (int32_t)(((int64_t)n_k + block - 1) / block);
   if (*nbq > PSA_MAX_BLOCKS || *nbk > PSA_MAX_BLOCKS)
     return fail(PSA_ERR_UNSUPPORTED, "%d x %d blocks exceed %d", *nbq, *nbk, PSA_MAX_BLOCKS);
-  // (work items, and blocks of both sides together, are 32-bit numbers)
-  if ((int64_t)batch * n_heads * ((int64_t)*nbq + *nbk) >= ((int64_t)1 << 31) - 8)
+  // (work items, and blocks of both sides together, are 32-bit numbers; of the two products the first may need 62 bits)
+  const int64_t most = ((int64_t)1 << 31) - 8, n_bh = (int64_t)batch * n_heads;
+  if (n_bh >= most || n_bh * ((int64_t)*nbq + *nbk) >= most)
     return fail(PSA_ERR_UNSUPPORTED, "too many work items");
   return PSA_OK;
 }

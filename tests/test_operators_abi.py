@@ -227,3 +227,19 @@ def test_a_stream_of_another_device_is_refused():
 
     with pytest.raises(ValueError, match="stream"):
         psa._on_device(torch.device("cuda", 0), Stream())
+
+
+HUGE = [(1 << 28, 2 ** 31 - 32, 10000, 10000), (1 << 30, 1 << 30, 1, 10000), (1 << 30, 2 ** 31 - 128, 10000, 1),
+        (2 ** 31 - 1, 2 ** 31 - 1, 1, 1), (2 ** 31 - 1, 1 << 29, 7936 * 64, 7936 * 64)]
+
+
+@pytest.mark.parametrize("batch,heads,n_q,n_k", HUGE)
+def test_products_of_batch_and_heads_past_64_bits(batch, heads, n_q, n_k):
+    """Sizes whose blocks 64 bits do not count are refused like smaller ones that are too many."""
+    L = _lib.lib()
+    for hk in (1, heads):
+        more = dict(batch=batch, heads=heads, n_q=n_q, n_k=n_k, x=kv(heads=hk))
+        assert select(**more) == mapped(**more) == mapped_bwd(**more) == UNSUPPORTED
+        assert L.psa_select_workspace_size(batch, heads, hk, 64, n_q, n_k, 64) == 0
+        assert L.psa_attention_map_bwd_workspace_size(batch, heads, hk, 64, n_q, n_k, 64) == 0
+    assert L.psa_attention_map_workspace_size(batch, heads, 64, n_q, n_k, 64) == 0
