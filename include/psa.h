@@ -329,7 +329,7 @@ typedef enum {
 typedef struct {
   void* x;
   int64_t stride_b, stride_h, stride_n;
-  int32_t n_heads;
+  int32_t n_heads;            /* at most 2^30 */
 } psa_rows_t;
 
 /* The rotation: N = frames * height * width + n_text tokens; channels of each axis (even, >= 0, together

@@ -264,6 +264,8 @@ psa_status_t run_planned(const void* q, const void* k, const void* v, void* o, i
   return PSA_OK;
 }
 
+constexpr int32_t kMaxRowHeads = 1 << 30;     // (the kernels step over the heads in 32 bits)
+
 // Whether no two rows share memory: of the axes with more than one place, in the order of their strides, each
 // steps over all that the smaller ones reach.
 bool rows_apart(const psa_rows_t& r, int32_t batch, int64_t n, int32_t head_dim) {
@@ -285,6 +287,7 @@ psa_status_t check_rows(const psa_rows_t& r, const char* what, int32_t batch, in
   if (!r.x) return fail(PSA_ERR_INVALID, "%s is NULL", what);
   if (!aligned(r.x, 16)) return fail(PSA_ERR_INVALID, "%s must be 16-byte aligned (%p)", what, r.x);
   if (r.n_heads < 1) return fail(PSA_ERR_INVALID, "%s: n_heads must be >= 1 (got %d)", what, r.n_heads);
+  if (r.n_heads > kMaxRowHeads) return fail(PSA_ERR_UNSUPPORTED, "%s: %d heads are too many", what, r.n_heads);
   if (r.stride_b % unit || r.stride_h % unit || r.stride_n % unit || r.stride_b < 0 || r.stride_h < 0 || r.stride_n < 0)
     return fail(PSA_ERR_INVALID, "%s: strides must be multiples of 16 bytes, not negative (%lld, %lld, %lld)", what,
                 (long long)r.stride_b, (long long)r.stride_h, (long long)r.stride_n);
@@ -730,8 +733,8 @@ size_t psa_qk_norm_rope_workspace_size(int32_t batch, int32_t n_heads, int32_t n
                                        int32_t head_dim, psa_grid_t grid, int32_t norm) {
   psa::Geometry g;
   const int32_t n_tensors = n_kv_heads > 0 ? 2 : 1;
-  if (!norm || batch < 1 || n_heads < 1 || n_kv_heads < 0 || (head_dim != 64 && head_dim != 128) ||
-      !rope_batch_fits(batch, n_tensors) || !grid_geometry(grid, 1, &g))
+  if (!norm || batch < 1 || n_heads < 1 || n_kv_heads < 0 || n_heads > kMaxRowHeads || n_kv_heads > kMaxRowHeads ||
+      (head_dim != 64 && head_dim != 128) || !rope_batch_fits(batch, n_tensors) || !grid_geometry(grid, 1, &g))
     return 0;
   psa::RopeArgs a = {};
   a.batch = batch;

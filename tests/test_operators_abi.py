@@ -243,3 +243,14 @@ def test_products_of_batch_and_heads_past_64_bits(batch, heads, n_q, n_k):
         assert L.psa_select_workspace_size(batch, heads, hk, 64, n_q, n_k, 64) == 0
         assert L.psa_attention_map_bwd_workspace_size(batch, heads, hk, 64, n_q, n_k, 64) == 0
     assert L.psa_attention_map_workspace_size(batch, heads, 64, n_q, n_k, 64) == 0
+
+
+@pytest.mark.parametrize("heads", [2 ** 30 + 1, 2 ** 31 - 40, 2 ** 31 - 16, 2 ** 31 - 1])
+def test_norm_rope_of_more_heads_than_32_bits_step_over(heads):
+    """The walk over the heads counts past the last of them."""
+    size = lambda *h: [_lib.lib().psa_qk_norm_rope_workspace_size(1, *h, d, _lib.grid_of(1, 1, n), 1) for d in (64, 128) for n in (1, 300)]
+    assert not any(size(heads, 0) + size(heads, heads) + size(2, heads))
+    assert all(0 < x < 2 ** 22 for x in size(2 ** 30, 0) + size(2 ** 30, 2 ** 30))
+    x = rows(heads=heads, h=0)
+    assert fwd(q=x) == fwd(k=x) == UNSUPPORTED
+    assert bwd(q=x) == bwd(k=x) == bwd(dq=x) == bwd(norm=0, q=x, dq=x) == UNSUPPORTED
