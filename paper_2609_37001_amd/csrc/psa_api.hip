@@ -39,6 +39,7 @@ bool grid_geometry(psa_grid_t grid, int32_t block, psa::Geometry* g) {
   if (grid.frames < 1 || grid.height < 1 || grid.width < 1 || grid.n_text < 0 || block < 1)
     return false;
   const int64_t hw = (int64_t)grid.height * grid.width;
+  if (hw >= ((int64_t)1 << 31)) return false;             // (times the frames it may not fit 64 bits)
   const int64_t n_video = hw * grid.frames;
   const int64_t n = n_video + grid.n_text;
   if (n + 2 * (int64_t)block >= ((int64_t)1 << 31)) return false;

@@ -254,3 +254,14 @@ def test_norm_rope_of_more_heads_than_32_bits_step_over(heads):
     x = rows(heads=heads, h=0)
     assert fwd(q=x) == fwd(k=x) == UNSUPPORTED
     assert bwd(q=x) == bwd(k=x) == bwd(dq=x) == bwd(norm=0, q=x, dq=x) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("grid", [(2 ** 30, 2 ** 20, 2 ** 14, 0), (2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1),
+                                  (2 ** 28, 2 ** 28, 2 ** 28, 77), (2 ** 16, 2 ** 24, 2 ** 24, 0), (5, 2 ** 31 - 1, 2 ** 31 - 1, 1)])
+def test_grids_of_more_tokens_than_64_bits_count(grid):
+    L = _lib.lib()
+    g = _lib.grid_of(*grid)
+    assert L.psa_num_blocks(g, 128) == -1 and L.psa_workspace_size(1, 2, g, 128) == 0
+    for d, axes in ((64, (24, 20, 20)), (128, (44, 42, 42))):
+        assert L.psa_qk_norm_rope_workspace_size(1, 12, 12, d, g, 1) == 0
+        assert fwd(d=d, r=rope(grid, axes=axes)) == INVALID
