@@ -296,7 +296,7 @@ static void rope_split(RopeArgs& a, int32_t d, int32_t groups, int32_t* head_gro
   const int64_t have = (int64_t)a.tiles * a.batch * a.n_tensors;
   const int32_t want = (int32_t)std::max<int64_t>(1, std::min<int64_t>((heads + step - 1) / step, groups / have));
   a.heads_per_group = ((heads + want - 1) / want + step - 1) / step * step;
-  *head_groups = (heads + a.heads_per_group - 1) / a.heads_per_group;
+  *head_groups = (heads - 1) / a.heads_per_group + 1;
 }
 
 // Workgroups that a launch aims at: eight of four waves on each of 256 CUs.  Fewer start fewer waves than hide the
