@@ -660,7 +660,7 @@ def _map_of(blockmap, q, n_k, block):
     shape = (q.shape[1], _blocks(q.shape[2], block), _blocks(n_k, block))
     if blockmap.device != q.device or tuple(blockmap.shape) not in (shape, (q.shape[0],) + shape):
         raise ValueError("blockmap must be %s or %s on the queries' device" % (shape, (q.shape[0],) + shape))
-    one = blockmap if blockmap.dim() == 3 else blockmap[0]
+    one = blockmap[0] if blockmap.dim() == 4 and q.shape[0] > 0 else blockmap
     if not one.is_contiguous():
         raise ValueError("the maps of a batch element must be contiguous")
     return blockmap.data_ptr(), blockmap.stride(0) if blockmap.dim() == 4 and q.shape[0] > 1 else 0

@@ -265,3 +265,16 @@ def test_grids_of_more_tokens_than_64_bits_count(grid):
     for d, axes in ((64, (24, 20, 20)), (128, (44, 42, 42))):
         assert L.psa_qk_norm_rope_workspace_size(1, 12, 12, d, g, 1) == 0
         assert fwd(d=d, r=rope(grid, axes=axes)) == INVALID
+
+
+def test_a_map_of_no_batch_elements_reaches_the_librarys_refusal():
+    import torch
+
+    import paper_2609_37001_amd as psa
+    q = torch.zeros(0, 2, 100, 64)
+    assert psa._map_of(torch.zeros(0, 2, 2, 3, dtype=torch.uint8), q, 150, 64)[1] == 0
+    for dims in ((2, 2, 3), (0, 2, 2, 3)):
+        psa._map_of(torch.zeros(dims, dtype=torch.uint8), q, 150, 64)
+    with pytest.raises(ValueError):
+        psa._map_of(torch.zeros(0, 2, 3, 2, dtype=torch.uint8), q, 150, 64)
+    assert mapped(batch=0) == mapped_bwd(batch=0) == select(batch=0) == INVALID
