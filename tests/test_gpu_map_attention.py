@@ -574,3 +574,25 @@ def test_values_that_are_not_finite_stay_where_they_are_kept(d, block, h, hk, nq
         assert torch.equal(got[i][:, :, rows != 2], ref[i][:, :, rows != 2])
     for i in (3, 4):
         assert torch.equal(got[i][:, :, keys != 4], ref[i][:, :, keys != 4])
+
+
+@pytest.mark.parametrize("d,block", SHAPES)
+def test_many_short_sequences(d, block):
+    """Far more query and key blocks than any other test has, in one list of each kernel's order: 256,000 of one block each."""
+    torch = gu.torch()
+    b, h, hk, n_q, n_k = 16000, 16, 8, 3, 2 * block + 5
+    rng = np.random.default_rng(81)
+    t = [torch.randn(b, m, n, d, device="cuda:0", dtype=torch.bfloat16) for m, n in ((h, n_q), (hk, n_k), (hk, n_k), (h, n_q))]
+    m = torch.from_numpy((rng.random((b, h, 1, 3)) < 0.6).astype(np.uint8)).to("cuda:0")
+    o, lse = psa.attention_map_fwd(*t[:3], m, block, return_lse=True)
+    got = psa.attention_map_bwd(t[3], *t[:3], o, lse, m, block)
+    sel, kept = psa.select_blocks(t[0], t[1], block, 2)
+    assert (kept == 2).all() and (sel.sum(3) == 2).all()
+    some = [0, 1, 4097, 8191, 12345, b - 2, b - 1]
+    q, k, v, do = (bits(x[some]) for x in t)
+    mn, on, ln = m[some].cpu().numpy(), bits(o[some]), lse[some].cpu().numpy()
+    check_forward(q, k, v, mn, block, d ** -0.5, on, ln, range(h))
+    check_backward(q, k, v, do, mn, block, d ** -0.5, on, ln, [x[some] for x in got], range(h))
+    for i, bi in enumerate(some):
+        for hi in range(h):
+            assert np.array_equal(sel[bi, hi].cpu().numpy(), selection.select_blocks(q[i, hi], k[i, hi // 2], block, 2))
